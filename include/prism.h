@@ -337,6 +337,130 @@ int prism_sparse_attn_varlen(const prism_params* params, const int32_t* cu_seqle
                              void* out_bf16, float* lse,
                              void* workspace, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------------------------
+ * Serving: rotary positions, a paged cache of keys and values, attention of new tokens over it.
+ *
+ * What follows a prefill.  The keys and values of a prompt are stored in pages with
+ * prism_cache_append; each later step (or chunk of a prompt) rotates and appends its own and attends over
+ * everything stored with prism_cache_attn.  Lengths, offsets and page tables are read on the device, so a
+ * captured graph serves batches whose lengths change between replays.
+ *
+ * prism_rows: a tensor [heads, tokens, head_dim] of bf16 whose last axis is contiguous and whose other two
+ * have strides of their own (in elements): the dense layout above (token_stride = d, head_stride = T * d), or
+ * the heads inside one projection [tokens, heads * d] (token_stride = heads * d, head_stride = d).  `data` is
+ * 16-byte aligned, strides are multiples of 8 and not negative; the stride of an axis of length one is not
+ * looked at.  The rows of an output must not overlap: PRISM_ERR_INVALID_ARG unless one of its strides steps over
+ * everything that the other axis spans.
+ * ---------------------------------------------------------------------------------- */
+typedef struct prism_rows {
+  void*   data;          /* device */
+  int64_t head_stride;   /* elements from a head to the next   */
+  int64_t token_stride;  /* elements from a token to the next  */
+} prism_rows;
+
+/* Rotary positions (Sec. 3.1 "Spectral Structure of RoPE") of the first rot_dim dims of a head; the dims behind them
+ * stay as they are.  Pair j = 0 .. rot_dim/2 - 1 turns by (position + freq.position_offset) * theta_j,
+ * theta_j = freq.base^(-2j/rot_dim), stretched by the yarn_* fields as in prism_rope_estimate (Llama-style scaling is the
+ * same map with alpha and beta as its low and high frequency factors):
+ *      x' = magnitude * (x cos(a) - y sin(a)),   y' = magnitude * (x sin(a) + y cos(a)).
+ * The angle is formed and reduced in double precision, cos and sin are evaluated in fp32. */
+#define PRISM_ROPE_INTERLEAVED 0   /* pair j = dims (2j, 2j + 1)            */
+#define PRISM_ROPE_HALF        1   /* pair j = dims (j, j + rot_dim / 2)    */
+typedef struct prism_rotary {
+  prism_rope freq;
+  int32_t rot_dim;       /* multiple of 16, 16 .. head_dim */
+  int32_t layout;        /* PRISM_ROPE_*                   */
+  float   magnitude;     /* > 0; 1 = a plain rotation (the attention factor of stretched frequencies goes here) */
+} prism_rotary;
+
+/* Rotates Q and K of n_tokens tokens.  positions: device int32 [n_tokens], NULL = token n has position n.
+ * q_out may be q_in and k_out may be k_in (same data and strides: in place); other overlaps are not allowed.
+ * n_kv_heads = 0 (k_in and k_out NULL) leaves K out, n_q_heads = 0 leaves Q out.
+ * PRISM_ROTATE_BACKWARD: the transposed map, which takes the gradients of the rotated tensors to those of the
+ * tensors before the rotation (angles -a, same magnitude).
+ * Errors: PRISM_ERR_INVALID_ARG, PRISM_ERR_UNSUPPORTED (head_dim not in {64,128,256}).  n_tokens = 0 does nothing. */
+#define PRISM_ROTATE_BACKWARD 1u
+int prism_rotate(const prism_rotary* rotary /* host */, int head_dim, int n_tokens, const int32_t* positions,
+                 int n_q_heads, const prism_rows* q_in /* host */, const prism_rows* q_out /* host */,
+                 int n_kv_heads, const prism_rows* k_in /* host */, const prism_rows* k_out /* host */,
+                 uint32_t flags, void* stream);
+
+/* A paged cache: K and V are [n_pages, n_kv_heads, page, head_dim], a page and head being contiguous.
+ * PRISM_CACHE_E4M3 holds a value x as the 8-bit float (e4m3, largest value 448) nearest to x / s with one scale s
+ * for each page and head, k_scale and v_scale [n_pages, n_kv_heads] floats.  prism_cache_append sets
+ * them to powers of two; prism_cache_attn takes any. */
+#define PRISM_CACHE_BF16 0
+#define PRISM_CACHE_E4M3 1
+typedef struct prism_cache {
+  void*   k;             /* device, 16-byte aligned */
+  void*   v;             /* device, 16-byte aligned */
+  float*  k_scale;       /* device; PRISM_CACHE_E4M3 only, else NULL */
+  float*  v_scale;
+  int64_t page_stride;   /* elements from a page to the next in k and in v, a multiple of 16; 0 = n_kv_heads * page * head_dim */
+  int32_t n_pages;
+  int32_t n_kv_heads;
+  int32_t page;          /* tokens of a page: 32, 64 or 128 */
+  int32_t head_dim;      /* 64, 128 or 256 */
+  int32_t dtype;         /* PRISM_CACHE_* */
+} prism_cache;
+
+/* The sequences of a call.  Sequence s has lengths[s] tokens once the call's are counted; its new tokens, the last ones,
+ * are the rows cu_tokens[s] .. cu_tokens[s+1]-1 of the call's q, k, v and out: new token i of n stands at position
+ * lengths[s] - n + i.  Token j of the sequence lies in page page_table[s * max_pages + j / page], place j % page.
+ * An entry outside 0 .. n_pages-1 (say -1) is no page: its tokens are not stored and not seen; entries behind the
+ * last token are not looked at.  Rows behind cu_tokens[n_seqs] are left as they were.  A position below 0 or beyond max_pages * page
+ * is not stored; a query there sees what lies in front of it.  No two sequences of one call may append to the same page. */
+typedef struct prism_batch {
+  int32_t n_seqs;
+  int32_t n_tokens;            /* rows of q, k, v and out */
+  int32_t max_tokens;          /* no sequence has more new tokens than this */
+  int32_t max_pages;           /* entries of a row of page_table */
+  const int32_t* cu_tokens;    /* device, [n_seqs + 1] ascending from 0; NULL = max_tokens for each sequence (n_tokens = n_seqs * max_tokens) */
+  const int32_t* lengths;      /* device, [n_seqs] */
+  const int32_t* page_table;   /* device, [n_seqs, max_pages] */
+} prism_batch;
+
+/* Stores K and V [n_kv_heads, n_tokens, d] of the new tokens.  `rotary` (may be NULL: K is stored as it is) rotates
+ * K by the tokens' positions on the way, and with q_in and q_out not NULL also Q [n_q_heads, n_tokens, d] (q_out may be
+ * q_in).  Values are rounded once, from fp32.
+ * PRISM_CACHE_E4M3: the scale of a page and head is the smallest power of two (at least 2^-120) with which all finite
+ * magnitudes of its tokens are at most 448.  A page that holds tokens of earlier calls keeps its scale while that is large
+ * enough; otherwise the scale grows and the values that are there move with it (exactly, unless they get into the smallest
+ * magnitudes of the format).  The first token of a page starts it anew, whatever its scale was.  NaN and infinity are stored
+ * as NaN.  Places behind the new tokens keep their bits.
+ * Errors: PRISM_ERR_INVALID_ARG, PRISM_ERR_UNSUPPORTED.  n_tokens = 0 does nothing.  Needs no workspace. */
+int prism_cache_append(const prism_cache* cache /* host */, const prism_batch* batch /* host */,
+                       const prism_rotary* rotary /* host, may be NULL */,
+                       const prism_rows* k /* host */, const prism_rows* v /* host */,
+                       int n_q_heads, const prism_rows* q_in /* host, may be NULL */, const prism_rows* q_out /* host */,
+                       void* stream);
+
+/* Attention of the new tokens over the cache (their own keys and values, appended before, among it).  For the
+ * new token at position p of its sequence and q-head hq (reading kv head hq / (n_q_heads / n_kv_heads)):
+ *    J = { j <= p : j has a page, and window = 0 or j > p - window or j < sinks }
+ *    o = sum_{j in J} softmax_J(scale * q . k_j)_j v_j       (bf16 in, fp32 accumulate, rounded to bf16)
+ * J empty (a sequence of length 0, say): o = 0, lse = -inf.  What lies in places outside J, infinities and NaN too, has
+ * no influence.
+ *   q, out : [n_q_heads, n_tokens, d]; out may be q.   lse : [n_q_heads, n_tokens] float natural-log sum-exp, or NULL.
+ * workspace: prism_cache_attn_workspace_bytes() bytes; it depends on the batch's n_seqs, n_tokens, max_tokens and
+ * max_pages only and carries nothing from call to call; calls that share one must not overlap.  The results do not depend
+ * on the order in which the device runs the parts of a call.
+ * Errors: PRISM_ERR_INVALID_ARG, PRISM_ERR_UNSUPPORTED, PRISM_ERR_WORKSPACE.  n_tokens = 0 does nothing. */
+typedef struct prism_cache_attn_params {
+  int32_t n_q_heads;
+  int32_t window;        /* 0 = all earlier tokens */
+  int32_t sinks;         /* first tokens that stay visible behind the window */
+  float   scale;         /* > 0; 0 = 1 / sqrt(head_dim) */
+} prism_cache_attn_params;
+
+int prism_cache_attn_workspace_bytes(const prism_cache* cache, const prism_batch* batch, int n_q_heads,
+                                     size_t* bytes /* host, out */);
+
+int prism_cache_attn(const prism_cache* cache /* host */, const prism_batch* batch /* host */,
+                     const prism_cache_attn_params* params /* host */,
+                     const prism_rows* q /* host */, const prism_rows* out /* host */, float* lse,
+                     void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -27,6 +27,11 @@ PRISM_FLAG_PAIR_KERNEL = 0x10000000
 PRISM_FLAG_GENERAL_KERNEL = 0x20000000
 PRISM_FLAG_STREAM_ONLY = 0x40000000
 PRISM_MAX_SEGMENTS = 8
+PRISM_ROPE_INTERLEAVED = 0
+PRISM_ROPE_HALF = 1
+PRISM_ROTATE_BACKWARD = 1
+PRISM_CACHE_BF16 = 0
+PRISM_CACHE_E4M3 = 1
 
 
 class PrismError(RuntimeError):
@@ -66,12 +71,40 @@ class prism_rope(ctypes.Structure):
                 ("yarn_alpha", ctypes.c_double), ("yarn_beta", ctypes.c_double)]
 
 
+class prism_rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("head_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64)]
+
+
+class prism_rotary(ctypes.Structure):
+    _fields_ = [("freq", prism_rope), ("rot_dim", ctypes.c_int32), ("layout", ctypes.c_int32),
+                ("magnitude", ctypes.c_float)]
+
+
+class prism_cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("page_stride", ctypes.c_int64), ("n_pages", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("page", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int32)]
+
+
+class prism_batch(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int32), ("n_tokens", ctypes.c_int32), ("max_tokens", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("cu_tokens", ctypes.c_void_p), ("lengths", ctypes.c_void_p),
+                ("page_table", ctypes.c_void_p)]
+
+
+class prism_cache_attn_params(ctypes.Structure):
+    _fields_ = [("n_q_heads", ctypes.c_int32), ("window", ctypes.c_int32), ("sinks", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
+
+
 EXPORTS = ("prism_version", "prism_status_string", "prism_estimate_workspace_bytes",
            "prism_estimate", "prism_estimate_static", "prism_estimate_bands", "prism_rope_estimate", "prism_block_scores",
            "prism_block_scores_bands", "prism_mask_to_csr", "prism_causal_csr", "prism_dense_csr",
            "prism_sparse_attn_workspace_bytes", "prism_sparse_attn", "prism_v_image",
            "prism_sparse_attn_pre", "prism_varlen_layout", "prism_estimate_varlen_workspace_bytes",
-           "prism_estimate_varlen", "prism_sparse_attn_varlen_workspace_bytes", "prism_sparse_attn_varlen")
+           "prism_estimate_varlen", "prism_sparse_attn_varlen_workspace_bytes", "prism_sparse_attn_varlen",
+           "prism_rotate", "prism_cache_append", "prism_cache_attn_workspace_bytes", "prism_cache_attn")
 
 
 def _load() -> ctypes.CDLL:
@@ -110,6 +143,12 @@ def _load() -> ctypes.CDLL:
     lib.prism_estimate_varlen.argtypes = [P, I32P, ctypes.c_int, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.prism_sparse_attn_varlen_workspace_bytes.argtypes = [P, I32P, ctypes.c_int, ctypes.POINTER(sz)]
     lib.prism_sparse_attn_varlen.argtypes = [P, I32P, ctypes.c_int, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    PR, PC, PT = ctypes.POINTER(prism_rows), ctypes.POINTER(prism_cache), ctypes.POINTER(prism_batch)
+    PY, i32 = ctypes.POINTER(prism_rotary), ctypes.c_int
+    lib.prism_rotate.argtypes = [PY, i32, i32, vp, i32, PR, PR, i32, PR, PR, ctypes.c_uint32, vp]
+    lib.prism_cache_append.argtypes = [PC, PT, PY, PR, PR, i32, PR, PR, vp]
+    lib.prism_cache_attn_workspace_bytes.argtypes = [PC, PT, i32, ctypes.POINTER(sz)]
+    lib.prism_cache_attn.argtypes = [PC, PT, ctypes.POINTER(prism_cache_attn_params), PR, PR, vp, vp, sz, vp]
     for name in EXPORTS[2:]:
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
@@ -345,6 +384,145 @@ def prism_sparse_attn_varlen(params: prism_params, cu_seqlens, q: torch.Tensor, 
                                             _ptr(row_ptr), _ptr(col_idx), _ptr(out), _ptr(lse),
                                             _ptr(workspace), workspace.numel(), _stream()),
            "prism_sparse_attn_varlen")
+
+
+# ---- serving: rotary positions, a paged cache, attention over it -------------------------------
+def _on_current(t: torch.Tensor, dtype, what: str) -> torch.Tensor:
+    if t.dtype != dtype or not t.is_cuda:
+        raise ValueError(f"{what}: expected a device tensor of {dtype}, got {t.dtype} on {t.device}")
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{what} is on {t.device}, calls go to the current device, cuda:{torch.cuda.current_device()}")
+    return t
+
+
+def _rows(t: Optional[torch.Tensor], what: str, shape=None) -> Optional[prism_rows]:
+    """[heads, tokens, d] bf16, contiguous in d, any strides of the library's in front"""
+    if t is None:
+        return None
+    _on_current(t, torch.bfloat16, what)
+    if t.dim() != 3 or (t.numel() > 0 and t.stride(2) != 1) or (shape is not None and t.shape != shape):
+        raise ValueError(f"{what}: expected [heads, tokens, head_dim]" + (f" = {tuple(shape)}" if shape is not None else "") +
+                         f" with a contiguous last axis, got {tuple(t.shape)} with strides {t.stride()}")
+    return prism_rows(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _dense(t: Optional[torch.Tensor], dtype, shape, what: str) -> Optional[int]:
+    if t is None:
+        return None
+    _on_current(t, dtype, what)
+    if t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{what}: expected a contiguous tensor {tuple(shape)}, got {tuple(t.shape)} with strides {t.stride()}")
+    return t.data_ptr()
+
+
+def _ref(s: Optional[ctypes.Structure]):
+    return ctypes.byref(s) if s is not None else None
+
+
+def make_rotary(base: float, rot_dim: int, layout: int = PRISM_ROPE_INTERLEAVED, position_offset: int = 0,
+                magnitude: float = 1.0, yarn_native_len: int = 0, yarn_scale: float = 1.0, yarn_alpha: float = 1.0,
+                yarn_beta: float = 32.0) -> prism_rotary:
+    return prism_rotary(make_rope(base, position_offset, yarn_native_len, yarn_scale, yarn_alpha, yarn_beta), rot_dim,
+                        layout, magnitude)
+
+
+def prism_rotate(rotary: prism_rotary, q_in: Optional[torch.Tensor], k_in: Optional[torch.Tensor],
+                 q_out: Optional[torch.Tensor], k_out: Optional[torch.Tensor],
+                 positions: Optional[torch.Tensor] = None, flags: int = 0) -> None:
+    some = q_in if q_in is not None else k_in
+    if some is None or (q_in is None) != (q_out is None) or (k_in is None) != (k_out is None):
+        raise ValueError("prism_rotate: expected Q, K or both, each with its output")
+    qi, ki = _rows(q_in, "q_in"), _rows(k_in, "k_in")
+    tokens, d = some.shape[1:]
+    if k_in is not None and k_in.shape[1:] != some.shape[1:]:
+        raise ValueError(f"q_in and k_in differ in tokens or head_dim: {tuple(q_in.shape)}, {tuple(k_in.shape)}")
+    qo = _rows(q_out, "q_out", q_in.shape) if qi is not None else None
+    ko = _rows(k_out, "k_out", k_in.shape) if ki is not None else None
+    _check(_load().prism_rotate(ctypes.byref(rotary), d, tokens, _dense(positions, torch.int32, (tokens,), "positions"),
+                                q_in.shape[0] if qi is not None else 0, _ref(qi), _ref(qo),
+                                k_in.shape[0] if ki is not None else 0, _ref(ki), _ref(ko), flags, _stream()),
+           "prism_rotate")
+
+
+def alloc_cache(n_pages: int, n_kv_heads: int, page: int, head_dim: int, dtype: int = PRISM_CACHE_BF16, device="cuda"):
+    """(k, v, k_scale, v_scale) of a cache; the scales are None in bf16"""
+    t = torch.float8_e4m3fn if dtype == PRISM_CACHE_E4M3 else torch.bfloat16
+    k, v = (torch.empty((n_pages, n_kv_heads, page, head_dim), dtype=t, device=device) for _ in range(2))
+    if dtype != PRISM_CACHE_E4M3:
+        return k, v, None, None
+    return k, v, *(torch.empty((n_pages, n_kv_heads), dtype=torch.float32, device=device) for _ in range(2))
+
+
+def make_cache(k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
+               v_scale: Optional[torch.Tensor] = None) -> prism_cache:
+    """Descriptor of a cache in tensors [n_pages, n_kv_heads, page, head_dim]; keeps them alive.  The pages of k and v may
+    be apart by the same stride, as in one tensor [n_pages, 2, n_kv_heads, page, head_dim]."""
+    if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.dtype not in (torch.bfloat16, torch.float8_e4m3fn):
+        raise ValueError(f"expected k and v [n_pages, n_kv_heads, page, head_dim] in bfloat16 or float8_e4m3fn, got "
+                         f"{tuple(k.shape)} {k.dtype} and {tuple(v.shape)} {v.dtype}")
+    n_pages, h_kv, page, d = k.shape
+    for t, what in ((k, "k"), (v, "v")):
+        _on_current(t, k.dtype, what)
+        if any(n > 1 and a != b for n, a, b in zip(t.shape[1:], t.stride()[1:], (page * d, d, 1))):
+            raise ValueError(f"{what}: the pages are contiguous [n_kv_heads, page, head_dim], got strides {t.stride()}")
+    if n_pages > 1 and k.stride(0) != v.stride(0):
+        raise ValueError(f"the pages of k and v lie {k.stride(0)} and {v.stride(0)} elements apart, expected the same")
+    e4m3 = k.dtype == torch.float8_e4m3fn
+    if e4m3 != (k_scale is not None) or e4m3 != (v_scale is not None):
+        raise ValueError("k_scale and v_scale belong to a cache in float8_e4m3fn, and only there")
+    c = prism_cache(k.data_ptr(), v.data_ptr(), _dense(k_scale, torch.float32, (n_pages, h_kv), "k_scale"),
+                    _dense(v_scale, torch.float32, (n_pages, h_kv), "v_scale"), k.stride(0) if n_pages > 1 else 0, n_pages,
+                    h_kv, page, d, PRISM_CACHE_E4M3 if e4m3 else PRISM_CACHE_BF16)
+    c._keep = (k, v, k_scale, v_scale)
+    return c
+
+
+def make_batch(lengths: torch.Tensor, page_table: torch.Tensor, max_tokens: int = 1,
+               cu_tokens: Optional[torch.Tensor] = None, n_tokens: Optional[int] = None) -> prism_batch:
+    """Descriptor of a batch; keeps its int32 device tensors alive.  Without cu_tokens every sequence has max_tokens new
+    tokens; with them n_tokens (rows of q, k, v and out) is given too."""
+    n = lengths.numel()
+    if page_table.dim() != 2 or page_table.shape[0] != n:
+        raise ValueError(f"expected page_table [{n}, max_pages], got {tuple(page_table.shape)}")
+    if cu_tokens is not None and n_tokens is None:
+        raise ValueError("cu_tokens lives on the device: n_tokens has to be given with it")
+    if cu_tokens is None and n_tokens not in (None, n * max_tokens):
+        raise ValueError(f"{n} sequences of {max_tokens} new tokens are not {n_tokens}")
+    b = prism_batch(n, n * max_tokens if cu_tokens is None else n_tokens, max_tokens, page_table.shape[1],
+                    _dense(cu_tokens, torch.int32, (n + 1,), "cu_tokens"), _dense(lengths, torch.int32, (n,), "lengths"),
+                    _dense(page_table, torch.int32, page_table.shape, "page_table"))
+    b._keep = (lengths, page_table, cu_tokens)
+    return b
+
+
+def prism_cache_append(cache: prism_cache, batch: prism_batch, rotary: Optional[prism_rotary], k: torch.Tensor,
+                       v: torch.Tensor, q_in: Optional[torch.Tensor] = None,
+                       q_out: Optional[torch.Tensor] = None) -> None:
+    kv = (cache.n_kv_heads, batch.n_tokens, cache.head_dim)
+    heads = 0 if q_in is None else q_in.shape[0]
+    q = (heads, batch.n_tokens, cache.head_dim)
+    _check(_load().prism_cache_append(ctypes.byref(cache), ctypes.byref(batch), _ref(rotary), _ref(_rows(k, "k", kv)),
+                                      _ref(_rows(v, "v", kv)), heads, _ref(_rows(q_in, "q_in", q)),
+                                      _ref(_rows(q_out, "q_out", q)), _stream()), "prism_cache_append")
+
+
+def prism_cache_attn_workspace_bytes(cache: prism_cache, batch: prism_batch, n_q_heads: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(_load().prism_cache_attn_workspace_bytes(ctypes.byref(cache), ctypes.byref(batch), n_q_heads, ctypes.byref(n)),
+           "prism_cache_attn_workspace_bytes")
+    return n.value
+
+
+def prism_cache_attn(cache: prism_cache, batch: prism_batch, q: torch.Tensor, out: torch.Tensor,
+                     lse: Optional[torch.Tensor], workspace: torch.Tensor, window: int = 0, sinks: int = 0,
+                     scale: float = 0.0) -> None:
+    heads = q.shape[0]
+    shape = (heads, batch.n_tokens, cache.head_dim)
+    params = prism_cache_attn_params(heads, window, sinks, scale)
+    _check(_load().prism_cache_attn(ctypes.byref(cache), ctypes.byref(batch), ctypes.byref(params),
+                                    _ref(_rows(q, "q", shape)), _ref(_rows(out, "out", shape)),
+                                    _dense(lse, torch.float32, shape[:2], "lse"), _ptr(workspace),
+                                    workspace.numel() * workspace.element_size(), _stream()), "prism_cache_attn")
 
 
 # ---- conveniences for callers holding numpy bf16 bit patterns --------------------------

@@ -10,7 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libprism.so")
-SOURCES = ["prism_estimate.hip", "prism_attn.hip"]
+SOURCES = ["prism_estimate.hip", "prism_cache.hip", "prism_cache_attn.hip", "prism_attn.hip"]
 # bench-only probes of the machine's achievable peaks (bench.py --peaks); not part of libprism
 PEAKS_LIB_PATH = os.path.join(HERE, "libprism_peaks.so")
 PEAKS_SOURCES = ["prism_peaks.hip"]
