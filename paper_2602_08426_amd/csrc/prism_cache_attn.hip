@@ -3,17 +3,29 @@
 // The rows of a (sequence, kv head) are its new tokens times the q-heads of the kv head: row r = token r / g, head r % g,
 // so that a tile of keys and values is read once for all of them.
 #include "prism_cache.h"
+#include "prism_tiles.h"
+
+#include <type_traits>
 
 namespace prism {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_rsrc(const char* base, int bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, bytes, 0x00020000);
-}
 // a value that is the same in all lanes, in a scalar register
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// Infinities and NaN among packed values: the top bits of theirs (bf16: an exponent of ones; e4m3: NaN, 0x7F and 0xFF), and the
+// word with zeros in their place.
+template <bool kE4m3>
+__device__ __forceinline__ uint32_t special_bits(uint32_t w) {
+  return kE4m3 ? ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u : ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
+}
+template <bool kE4m3>
+__device__ __forceinline__ uint32_t without_specials(uint32_t w) {
+  const uint32_t n = special_bits<kE4m3>(w);
+  return w & ~(kE4m3 ? (n >> 7) * 0xFFu : (n >> 15) * 0xFFFFu);
+}
 
 // What the kernels need to know of a call.
 struct AttnCall {
@@ -24,16 +36,17 @@ struct AttnCall {
   int h, g;                // q-heads, of a kv head
   int window, sinks;
   float scale;             // of the scores, times log2(e)
+  int step_rows;           // a sequence and kv head of at most so many rows is step_kernel's, others chunk_kernel's
 };
 
 // The keys that some row of a sequence (or of a part of its new tokens) sees, in tiles of kTile tokens: the tiles [0, sink)
 // and [low, end).
-constexpr int kTile = 32;
 struct KeyRange {
   int sink, low, end;
   __device__ __forceinline__ int count() const { return sink + end - low; }
   __device__ __forceinline__ int tile(int i) const { return i < sink ? i : low + i - sink; }
 };
+template <int kTile>
 __device__ __forceinline__ KeyRange key_range(const AttnCall& a, int first_pos, int last_pos) {
   const int keys = min(last_pos + 1, a.batch.max_pages << a.cache.page_shift);
   KeyRange k = {0, 0, 0};
@@ -44,11 +57,6 @@ __device__ __forceinline__ KeyRange key_range(const AttnCall& a, int first_pos, 
     k.sink = min((min(a.sinks, keys) + kTile - 1) / kTile, k.low);
   }
   return k;
-}
-__device__ __forceinline__ KeyRange keys_of(const AttnCall& a, const SeqRows& r) {
-  const int n = min(r.n, a.batch.each);
-  if (n == 0) return KeyRange{0, 0, 0};
-  return key_range(a, r.length - r.n, r.length - r.n + n - 1);
 }
 
 // =====================================================================================
@@ -68,8 +76,14 @@ __device__ __forceinline__ KeyRange keys_of(const AttnCall& a, const SeqRows& r)
 // transposes 8 x 8 values inside the lane.  The dims of a k-step of S^T are any, as long as Q has the same: a lane's are where its
 // 16-byte pieces lie.
 // =====================================================================================
-constexpr int kStepWaves = 4;
+constexpr int kTile = 32, kStepWaves = 4;
 constexpr int kStepThreads = kStepWaves * 64;
+
+__device__ __forceinline__ KeyRange keys_of(const AttnCall& a, const SeqRows& r) {
+  const int n = min(r.n, a.batch.each);
+  if (n == 0 || (int64_t)n * a.g > a.step_rows) return KeyRange{0, 0, 0};
+  return key_range<kTile>(a, r.length - r.n, r.length - r.n + n - 1);
+}
 
 // Prefix sums over the units of all sequences, 256 at a time.
 __device__ __forceinline__ int step_units(const AttnCall& a, int s) {
@@ -240,8 +254,8 @@ __global__ __launch_bounds__(kStepThreads, D == 256 || MT > 1 ? 1 : 2) void step
           }
           const int64_t off = max(x.page, 0) * a.cache.page_stride + (int64_t)(kv * a.cache.page + (tok & (a.cache.page - 1))) * kRow;
           const int bytes = x.page < 0 ? 0 : min(kTile, r.length - tok) * kRow;   // what lies behind the last token reads as zero
-          x.k = tile_rsrc(a.cache.k + off, bytes);
-          x.v = tile_rsrc(a.cache.v + off, bytes);
+          x.k = make_rsrc(a.cache.k + off, bytes);
+          x.v = make_rsrc(a.cache.v + off, bytes);
           return x;
         };
         u32x4 kw[C::kKLoads];
@@ -296,7 +310,7 @@ __global__ __launch_bounds__(kStepThreads, D == 256 || MT > 1 ? 1 : 2) void step
           }
         };
         // A operand of O^T, dims lane_dim(., d): the lane's 8 keys of that dim
-        auto v_frag = [&](const uint32_t(&vw)[8][C::kVWords], int d) __attribute__((always_inline)) {
+        auto v_frag = [&](int d) __attribute__((always_inline)) {
           u32x4 w;
 #pragma unroll
           for (int p = 0; p < 4; ++p) {                   // keys 2p, 2p + 1
@@ -345,8 +359,8 @@ __global__ __launch_bounds__(kStepThreads, D == 256 || MT > 1 ? 1 : 2) void step
           // Without branches: from && and || the compiler (AMD clang 22) made control flow around the writes of single score
           // elements, and lost one of them.
           const int window = a.window > 0 ? a.window : 0x40000000;
-          auto sees = [&](int key, int newest, int oldest) __attribute__((always_inline)) {   // by a row in between
-            return (now.page >= 0) & (key <= newest) & ((key > oldest - window) | (key < a.sinks));
+          auto sees = [&](int key, int pos) __attribute__((always_inline)) {
+            return (now.page >= 0) & (key <= pos) & ((key > pos - window) | (key < a.sinks));
           };
           bool special = false;
           if (!whole) {
@@ -354,23 +368,20 @@ __global__ __launch_bounds__(kStepThreads, D == 256 || MT > 1 ? 1 : 2) void step
             for (int x = 0; x < MT; ++x)
 #pragma unroll
               for (int j = 0; j < 8; ++j)
-                sc[x][j >> 2][j & 3] = sees(first + 8 * qd + j, row_pos[x], row_pos[x]) ? sc[x][j >> 2][j & 3] : -INFINITY;
-            // 0 * NaN is NaN: the values of keys that no row sees become zeros; a key that only some rows see and that
-            // holds an infinity or NaN sends the tile to the token by token form below
+                sc[x][j >> 2][j & 3] = sees(first + 8 * qd + j, row_pos[x]) ? sc[x][j >> 2][j & 3] : -INFINITY;
+            // 0 * NaN is NaN: infinities and NaN among the values leave the product and are added where they are seen
             uint32_t bad = 0;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const bool some = sees(first + 8 * qd + j, pos_last, pos0);
+            for (int j = 0; j < 8; ++j)
 #pragma unroll
-              for (int w = 0; w < C::kVWords; ++w) {
-                vw[j][w] = some ? vw[j][w] : 0u;
-                if constexpr (kE4m3)                      // a byte 0x7F or 0xFF
-                  bad |= ((vw[j][w] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
-                else                                      // an exponent of ones
-                  bad |= ((vw[j][w] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
-              }
+              for (int w = 0; w < C::kVWords; ++w) bad |= special_bits<kE4m3>(vw[j][w]);
+            special = __builtin_amdgcn_ballot_w64(bad != 0) != 0;
+            if (special) {
+#pragma unroll
+              for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int w = 0; w < C::kVWords; ++w) vw[j][w] = without_specials<kE4m3>(vw[j][w]);
             }
-            special = n > 1 && __builtin_amdgcn_ballot_w64(bad != 0) != 0;
           }
 
           // ---- online softmax: a row is in the lanes m, m + 16, m + 32, m + 48 ----
@@ -410,34 +421,32 @@ __global__ __launch_bounds__(kStepThreads, D == 256 || MT > 1 ? 1 : 2) void step
           }
 
           // ---- O^T += V^T P^T ----
-          if (!special) {
 #pragma unroll
-            for (int d = 0; d < C::kDTiles; ++d) {
-              const bf16x8 f = v_frag(vw, d);
+          for (int d = 0; d < C::kDTiles; ++d) {
+            const bf16x8 f = v_frag(d);
 #pragma unroll
-              for (int x = 0; x < MT; ++x) o[x][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, pf[x], o[x][d], 0, 0, 0);
-            }
-          } else {
+            for (int x = 0; x < MT; ++x) o[x][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, pf[x], o[x][d], 0, 0, 0);
+          }
+          if (special) {
+            // p > 0 times an infinity or NaN is that
+            const int there = now.page < 0 ? 0 : min(kTile, r.length - first);
+            const char* vp = a.cache.v + max(now.page, 0) * a.cache.page_stride + (int64_t)(kv * a.cache.page + (first & (a.cache.page - 1))) * kRow;
 #pragma unroll 1
-            for (int pos = pos0; pos <= pos_last; ++pos) {
-              uint32_t seen[8][C::kVWords];
+            for (int j = 0; j < there; ++j)
 #pragma unroll
-              for (int j = 0; j < 8; ++j) {
-                const bool s = sees(first + 8 * qd + j, pos, pos);
+              for (int d = 0; d < C::kDTiles; ++d)
 #pragma unroll
-                for (int w = 0; w < C::kVWords; ++w) seen[j][w] = s ? vw[j][w] : 0u;
-              }
+                for (int e = 0; e < 4; ++e) {
+                  const char* vq = vp + j * kRow + lane_dim<D>(4 * qd + e, d) * C::kElem;
+                  float y;
+                  if constexpr (kE4m3)
+                    y = __builtin_amdgcn_cvt_f32_fp8(*reinterpret_cast<const uint8_t*>(vq), 0);
+                  else
+                    y = bf16_bits_to_float(*reinterpret_cast<const uint16_t*>(vq));
+                  const bool odd = !(fabsf(y) < INFINITY);
 #pragma unroll
-              for (int d = 0; d < C::kDTiles; ++d) {
-                const bf16x8 f = v_frag(seen, d);
-#pragma unroll
-                for (int x = 0; x < MT; ++x) {
-                  const f32x4 y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, pf[x], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-                  for (int e = 0; e < 4; ++e) o[x][d][e] = row_pos[x] == pos ? o[x][d][e] + y[e] : o[x][d][e];
+                  for (int x = 0; x < MT; ++x) o[x][d][e] = odd & sees(first + j, row_pos[x]) ? o[x][d][e] + y : o[x][d][e];
                 }
-              }
-            }
           }
           if (more) {
             load_v(next);
@@ -525,7 +534,8 @@ __global__ __launch_bounds__(kStepThreads) void combine_kernel(AttnCall a, StepW
   total *= h_kv;
   const int64_t W = shares(total, workgroups);
   const SeqRows r = seq_rows(a.batch, s);
-  const int R = min(r.n, a.batch.each) * a.g;
+  const int64_t rows = (int64_t)min(r.n, a.batch.each) * a.g;
+  const int R = rows > a.step_rows ? 0 : (int)rows;
   // the workgroup of unit x: the largest w with w * total / W <= x
   const int w0 = units > 0 ? (int)(((first + 1) * W - 1) / total) : 0;
   const int w1 = units > 0 ? (int)(((first + units) * W - 1) / total) : 0;
@@ -575,84 +585,486 @@ __global__ __launch_bounds__(kStepThreads) void combine_kernel(AttnCall a, StepW
   }
 }
 
-// One workgroup for a new token and a q-head: 256 keys at a time, one a thread, then their values by dims.
+// =====================================================================================
+// Chunks: many rows per sequence and kv head, bound by the matrix cores.
+//
+// A workgroup has 128 rows of a (sequence, kv head), 32 for each of its four waves, and goes through the keys that they see in
+// tiles of 64, K and V in two LDS buffers each: the next tile is requested while this one is used.  Formulation and tile
+// layout are those of the block-sparse kernel: S^T = K Q^T and O^T += V^T P^T with 32x32x16 MFMAs, a row in two lanes, V transposed
+// on the way from LDS.  bf16 pages are copied to LDS asynchronously; e4m3 pages pass through registers, where they
+// become bf16 once for the four waves (their scales go to the scores and the probabilities in fp32).
+// Rows of a kv head's q-heads lie side by side, so the 128 rows are 128 / g tokens and the diagonal costs little.
+// Where the row tiles are few, each is cut into `splits` parts of its keys, and chunk_combine_kernel joins them.
+// =====================================================================================
+constexpr int kChunkRows = 128, kChunkKeys = 64, kChunkThreads = 256;
+
+struct ChunkWs {
+  float* part;             // [workgroups][128][D] unscaled sums
+  float2* stats;           // [workgroups][128]
+};
+// Where a workgroup's rows are: kv head, row tile of all sequences, part.  Workgroups go round the eight XCDs; those of an XCD
+// get the same kv heads, whose keys then stay in its L2.  Later row tiles, which see more keys, first.
+struct ChunkPlace {
+  int kv, slot, split;
+};
+__device__ __forceinline__ ChunkPlace chunk_place(int b, int h_kv, int slots, int splits) {
+  ChunkPlace p;
+  if (8 % h_kv == 0) {                                    // 8 / h_kv XCDs share a kv head
+    const int share = 8 / h_kv, x = b & 7;
+    p.kv = x / share;
+    const int i = (b >> 3) * share + x % share;
+    p.slot = i / splits;
+    p.split = i % splits;
+  } else if (h_kv % 8 == 0) {
+    const int i = b >> 3, per = slots * splits;
+    p.kv = (b & 7) + 8 * (i / per);
+    p.slot = i % per / splits;
+    p.split = i % splits;
+  } else {
+    p.kv = b % h_kv;
+    p.slot = b / h_kv / splits;
+    p.split = b / h_kv % splits;
+  }
+  p.slot = slots - 1 - p.slot;
+  return p;
+}
+__host__ __device__ inline int chunk_grid(int h_kv, int slots, int splits) {
+  const int share = 8 % h_kv == 0 ? 8 / h_kv : 1;
+  return (slots * splits + share - 1) / share * share * h_kv;
+}
+// The rows of a slot; rows == 0: none, or not this kernel's.
+struct ChunkRows {
+  SeqRows r;
+  int s, row0, rows;       // first row, rows of the sequence
+};
+__device__ __forceinline__ ChunkRows chunk_rows(const AttnCall& a, int slot) {
+  ChunkRows c;
+  c.s = uniform(seq_at(a.batch, slot, a.g, 7, 1));
+  c.r = seq_rows(a.batch, c.s);
+  c.r.row0 = uniform(c.r.row0);
+  c.r.n = uniform(c.r.n);
+  c.r.length = uniform(c.r.length);
+  c.row0 = (slot - (int)((((int64_t)c.r.row0 * a.g) >> 7) + c.s)) * kChunkRows;
+  const int rows = min(c.r.n, a.batch.each) * a.g;
+  c.rows = rows > a.step_rows && c.row0 >= 0 && c.row0 < rows ? rows : 0;
+  return c;
+}
+
 template <int D, bool kE4m3>
-__global__ __launch_bounds__(256) void cache_attn_simple_kernel(Rows q, Rows out, float* __restrict__ lse, CacheView cache,
-                                                                BatchView batch, int h, int window, int sinks, float scale) {
-  __shared__ float s_q[D], s_p[256], s_red[8];
-  __shared__ int s_id[256];
-  const int64_t token = blockIdx.x;
-  const int hq = blockIdx.y, kv = hq / (h / cache.h_kv), t = threadIdx.x;
-  const int s = seq_at(batch, (int)token, 1, 0, 0);
-  const SeqRows r = seq_rows(batch, s);
-  const int i = (int)token - r.row0;
-  if (i < 0 || i >= r.n || i >= batch.each) return;
-  const int pos = r.length - r.n + i;
-  for (int d = t; d < D; d += 256) s_q[d] = bf16_bits_to_float(q.p[hq * q.head + token * q.token + d]);
-  __syncthreads();
-  const int end = min(pos + 1, batch.max_pages << cache.page_shift);
-  const int low = window > 0 ? max(pos - window + 1, 0) : 0;
-  float m = -INFINITY, l = 0.f, o = 0.f;
-  for (int j0 = 0; j0 < end; j0 += 256) {
-    if (j0 >= sinks && j0 + 256 <= low) continue;
-    const int j = j0 + t;
-    int id = -1;
-    if (j < end && (j >= low || j < sinks)) id = batch.table[(int64_t)s * batch.max_pages + (j >> cache.page_shift)];
-    const bool sees = id >= 0 && id < cache.n_pages;
-    float x = -INFINITY;
-    if (sees) {
-      const char* row = cache.k + id * cache.page_stride + ((int64_t)kv * cache.page + (j & (cache.page - 1))) * (D * (kE4m3 ? 1 : 2));
-      x = 0.f;
-      for (int d = 0; d < D; d += 4) {
+__global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(AttnCall a, ChunkWs ws, int slots, int splits) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  constexpr int KS = D / 16, DT = D / 32, KT = kChunkKeys / 32;
+  constexpr int kRow = D * 2, kTileBytes = kChunkKeys * kRow, kSlab = 32 * kRow;
+  constexpr int kPieces = D / 32, kHalf = kPieces / 2;    // 16-byte pieces of a thread, of 32 keys
+  constexpr int kCpr = D / 8, kRp = kChunkThreads / kCpr; // pieces of a row, rows of a piece of all threads
+  constexpr int kWide = kE4m3 ? D / 64 : 0;               // e4m3: 16-byte loads of a thread
+  __shared__ __attribute__((aligned(16))) char lds_k[2 * kTileBytes];
+  __shared__ __attribute__((aligned(16))) char lds_v[2 * kTileBytes];
+  __shared__ int s_special[2][4];
+  const int h_kv = a.cache.h_kv;
+  const ChunkPlace at = chunk_place(blockIdx.x, h_kv, slots, splits);
+  if (at.slot < 0) return;
+  const ChunkRows c = chunk_rows(a, at.slot);
+  if (c.rows == 0) return;
+  const int t = threadIdx.x, lane = t & 63, wave = uniform(t >> 6), l32 = lane & 31, hf = lane >> 5;
+  const int kv = at.kv, pos0 = c.r.length - c.r.n;
+  const int last_row = min(c.row0 + kChunkRows, c.rows) - 1;
+  const int wg_first = pos0 + c.row0 / a.g, wg_last = pos0 + last_row / a.g;
+  const KeyRange keys = key_range<kChunkKeys>(a, wg_first, wg_last);
+  const int c0 = (int)((int64_t)keys.count() * at.split / splits), c1 = (int)((int64_t)keys.count() * (at.split + 1) / splits);
+
+  // this wave's rows
+  const int wave_row0 = c.row0 + wave * 32, row = min(wave_row0 + l32, c.rows - 1);
+  const bool idle = wave_row0 >= c.rows;
+  const int tok = row / a.g, hq = kv * a.g + row - tok * a.g, row_pos = pos0 + tok;
+  const int pos_first = pos0 + wave_row0 / a.g, pos_last = pos0 + min(wave_row0 + 31, c.rows - 1) / a.g;
+  bf16x8 qf[KS];
+  {
+    const uint16_t* qp = a.q.p + (int64_t)hq * a.q.head + (int64_t)(c.r.row0 + tok) * a.q.token + hf * 8;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8*>(qp + ks * 16);
+  }
+  if (D > 128) {                                          // read by the MFMAs only: from AGPRs, in place
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+a"(qf[ks]));
+  }
+
+  // offsets: this lane's reads inside a slab of 32 rows, its pieces inside 32 keys of a page
+  int koff[KS], voff[D > 128 ? 4 : DT];
+  constexpr int kGroups = D > 128 ? 4 : DT;
+#pragma unroll
+  for (int st = 0; st < KS; ++st) koff[st] = l32 * kRow + (((2 * st + hf) ^ k_row_swizzle<D>(l32)) << 4);
+#pragma unroll
+  for (int i = 0; i < kGroups; ++i) {
+    const int key = 4 * hf + ((lane >> 2) & 3);
+    voff[i] = key * kRow + ((i ^ v_row_swizzle<D>(key)) << 6) + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+  }
+  int k_lane[2], v_lane[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int r = i * kRp + t / kCpr;
+    k_lane[i] = r * kRow + (((t % kCpr) ^ k_row_swizzle<D>(r)) << 4);
+    v_lane[i] = r * kRow + (((t % kCpr) ^ (v_row_swizzle<D>(r) << 2)) << 4);
+  }
+
+  // ---- tiles: entries of the page table (and scales) held 64 a time, one a lane ----
+  const int32_t* table = a.batch.table + (int64_t)c.s * a.batch.max_pages;
+  int held_from = -64, held = 0;
+  float held_ks = 0.f, held_vs = 0.f;
+  struct Half {
+    int page;                                             // < 0: none
+    float ks, vs;
+  };
+  struct Tile {
+    int first;                                            // its first key
+    Half half[2];
+  };
+  // halves of the tile that is being requested
+  TileRsrc krs[2], vrs[2];
+  const char *k_at[2], *v_at[2];
+  int half_bytes[2];
+  auto locate = [&](int list_at) __attribute__((always_inline)) {
+    Tile x;
+    x.first = keys.tile(list_at) * kChunkKeys;
+#pragma unroll
+    for (int hv = 0; hv < 2; ++hv) {
+      const int tk = x.first + 32 * hv, e = tk >> a.cache.page_shift;
+      if ((unsigned)(e - held_from) >= 64u) {
+        held_from = e;
+        const int mine = e + lane;
+        held = mine < a.batch.max_pages ? table[mine] : -1;
+        if (held >= a.cache.n_pages) held = -1;
         if (kE4m3) {
-          const int w = *reinterpret_cast<const int*>(row + d);
-          const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
-          x += s_q[d] * a[0] + s_q[d + 1] * a[1] + s_q[d + 2] * b[0] + s_q[d + 3] * b[1];
-        } else {
-          const uint2 w = *reinterpret_cast<const uint2*>(row + 2 * d);
-          x += s_q[d] * __uint_as_float(w.x << 16) + s_q[d + 1] * __uint_as_float(w.x & 0xFFFF0000u) +
-               s_q[d + 2] * __uint_as_float(w.y << 16) + s_q[d + 3] * __uint_as_float(w.y & 0xFFFF0000u);
+          const int64_t sc = (int64_t)max(held, 0) * h_kv + kv;
+          held_ks = a.cache.k_scale[sc];
+          held_vs = a.cache.v_scale[sc];
         }
       }
-      if (kE4m3) x *= cache.k_scale[(int64_t)id * cache.h_kv + kv];
-      x *= scale;
-    }
-    float top = wave_max(x);
-    if ((t & 63) == 0) s_red[t >> 6] = top;
-    __syncthreads();
-    top = fmaxf(m, fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3])));
-    const float base = top == -INFINITY ? 0.f : top;
-    const float p = sees ? expf(x - base) : 0.f;
-    const float sum = wave_sum(p);
-    if ((t & 63) == 0) s_red[4 + (t >> 6)] = sum;
-    s_p[t] = p;
-    s_id[t] = sees ? id : -1;
-    __syncthreads();
-    const float keep = expf(m - base);
-    l = l * keep + (s_red[4] + s_red[5] + s_red[6] + s_red[7]);
-    m = top;
-    if (t < D) {
-      o *= keep;
-      for (int i2 = 0; i2 < 256; ++i2) {
-        const int key = s_id[i2];
-        if (key < 0) continue;
-        const int64_t at = key * cache.page_stride + ((int64_t)kv * cache.page + ((j0 + i2) & (cache.page - 1))) * (D * (kE4m3 ? 1 : 2));
-        float v;
-        if (kE4m3)
-          v = __builtin_amdgcn_cvt_pk_f32_fp8((int)*reinterpret_cast<const uint8_t*>(cache.v + at + t), false)[0] *
-              cache.v_scale[(int64_t)key * cache.h_kv + kv];
-        else
-          v = bf16_bits_to_float(*reinterpret_cast<const uint16_t*>(cache.v + at + 2 * t));
-        o += s_p[i2] * v;
+      Half& y = x.half[hv];
+      y.page = __builtin_amdgcn_readlane(held, e - held_from);
+      if (kE4m3) {
+        y.ks = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, held_ks), e - held_from));
+        y.vs = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, held_vs), e - held_from));
+      }
+      constexpr int kPageRow = kE4m3 ? D : kRow;
+      const int64_t off = max(y.page, 0) * a.cache.page_stride + (int64_t)(kv * a.cache.page + (tk & (a.cache.page - 1))) * kPageRow;
+      // what lies behind the last token, or in no page, reads as zero
+      const int bytes = y.page < 0 ? 0 : max(min(32, c.r.length - tk), 0) * kPageRow;
+      if constexpr (kE4m3) {
+        k_at[hv] = a.cache.k + off;
+        v_at[hv] = a.cache.v + off;
+        half_bytes[hv] = bytes;
+      } else {
+        krs[hv] = make_tile_rsrc(a.cache.k + off, bytes);
+        vrs[hv] = make_tile_rsrc(a.cache.v + off, bytes);
       }
     }
-    __syncthreads();
+    return x;
+  };
+  const int wave_base = t & ~63;
+  // piece i of the tile in krs / vrs, to buffer b
+  auto copy_k = [&](int i, int b) __attribute__((always_inline)) {
+    const int j = i % kHalf;
+    async_piece(krs[i / kHalf], k_lane[j & 1], (j & 2) * kRp * kRow, (uint32_t)(size_t)lds_k + b * kTileBytes + (i * kChunkThreads + uniform(wave_base)) * 16);
+  };
+  auto copy_v = [&](int i, int b) __attribute__((always_inline)) {
+    const int j = i % kHalf;
+    async_piece(vrs[i / kHalf], v_lane[j & 1], (j & 2) * kRp * kRow, (uint32_t)(size_t)lds_v + b * kTileBytes + (i * kChunkThreads + uniform(wave_base)) * 16);
+  };
+  // e4m3: 16 values a piece, through registers
+  u32x4 kx[kWide > 0 ? kWide : 1], vx[kWide > 0 ? kWide : 1];
+  constexpr int kWideCpr = D / 16, kWideRp = kChunkThreads / kWideCpr;    // rows of a piece of all threads: 64, 32, 16
+  auto request = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kWide; ++i) {
+      const int r = i * kWideRp + t / kWideCpr;           // of the tile
+      const int hv = kWideRp == 64 ? uniform(r >> 5) : i * kWideRp / 32;
+      const int off = (r & 31) * D + (t % kWideCpr) * 16;
+      const int bytes = hv ? half_bytes[1] : half_bytes[0];
+      kx[i] = __builtin_amdgcn_raw_buffer_load_b128(make_rsrc(hv ? k_at[1] : k_at[0], bytes), off, 0, 0);
+      vx[i] = __builtin_amdgcn_raw_buffer_load_b128(make_rsrc(hv ? v_at[1] : v_at[0], bytes), off, 0, 0);
+    }
+  };
+  auto deliver = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kWide; ++i) {
+      const int r = i * kWideRp + t / kWideCpr, ch = 2 * (t % kWideCpr);
+#pragma unroll
+      for (int hv = 0; hv < 2; ++hv) {
+        u32x4 kw, vw;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t k8 = kx[i][2 * hv + (e >> 1)], v8 = vx[i][2 * hv + (e >> 1)];
+          kw[e] = __builtin_bit_cast(uint32_t, (e & 1) ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(k8, 1.0f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(k8, 1.0f, false));
+          vw[e] = __builtin_bit_cast(uint32_t, (e & 1) ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v8, 1.0f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v8, 1.0f, false));
+        }
+        *reinterpret_cast<u32x4*>(lds_k + b * kTileBytes + r * kRow + (((ch + hv) ^ k_row_swizzle<D>(r)) << 4)) = kw;
+        *reinterpret_cast<u32x4*>(lds_v + b * kTileBytes + r * kRow + (((ch + hv) ^ (v_row_swizzle<D>(r) << 2)) << 4)) = vw;
+      }
+    }
+  };
+  // A operand of O^T: dims 32*dt .. +31, keys 16*st + 8*(j/4) + 4*hf + j%4
+  auto v_frag = [&](int dt, int st, int b) __attribute__((always_inline)) {
+    typedef __attribute__((address_space(3))) bf16x4* lv4_t;
+    const char* p = lds_v + b * kTileBytes + voff[dt % kGroups] + (dt / kGroups) * (kGroups * 64) + st * (16 * kRow);
+    const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lv4_t)p), y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lv4_t)(p + 8 * kRow));
+    return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+
+  f32x16 o[DT];
+#pragma unroll
+  for (int i = 0; i < DT; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
+  float m_run = -INFINITY, l_run = 0.f;
+  const int window = a.window > 0 ? a.window : 0x40000000;
+
+  Tile now = {}, next = {};
+  // tile `now` in buffer kBuf; with `more` the tile in `next`, located here, goes to the other one
+  auto step = [&](auto buf_tag, int list_at) __attribute__((always_inline)) {
+    constexpr int kBuf = decltype(buf_tag)::value;
+    const bool more = list_at + 1 < c1;
+    if (more) next = locate(list_at + 1);
+    if (kE4m3 && more) request();
+    const int first = now.first, last = first + kChunkKeys - 1;
+    const bool none = idle || first > pos_last || (last <= pos_first - window && first >= a.sinks);
+    bf16x8 pf[KT][2];
+    constexpr int kDepth = 8;
+    if (none) {
+      if (!kE4m3 && more) {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) copy_k(i, 1 - kBuf);
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) copy_v(i, 1 - kBuf);
+      }
+    } else {
+      f32x16 sc[KT];
+      {
+        constexpr int kSteps = KT * KS, kEvery = kSteps / (2 * kPieces);
+        static_assert(kSteps >= kDepth && kSteps % (2 * kPieces) == 0, "pieces between the MFMAs");
+        const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        bf16x8 fr[kDepth];
+#pragma unroll
+        for (int i = 0; i < kDepth; ++i) fr[i] = *reinterpret_cast<const bf16x8*>(lds_k + kBuf * kTileBytes + (i % KT) * kSlab + koff[i / KT]);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+          const int kt = i % KT, ks = i / KT;
+          sc[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[i % kDepth], qf[ks], ks == 0 ? zero16 : sc[kt], 0, 0, 0);
+          if (i + kDepth < kSteps) {
+            const int j = i + kDepth;
+            fr[i % kDepth] = *reinterpret_cast<const bf16x8*>(lds_k + kBuf * kTileBytes + (j % KT) * kSlab + koff[j / KT]);
+          }
+          if (!kE4m3 && i % kEvery == 0) {
+            const int p = i / kEvery;
+            if (more) {
+              if (p < kPieces) copy_k(p, 1 - kBuf); else copy_v(p - kPieces, 1 - kBuf);
+            }
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      // ---- what a row sees: all of the tile, or each key for itself (without branches, as in step_kernel) ----
+      const bool whole = ((now.half[0].page | now.half[1].page) >= 0) & (last <= pos_first) & ((first > pos_last - window) | (last < a.sinks));
+      if (!whole) {
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int key = first + kt * 32 + 8 * (r >> 2) + 4 * hf + (r & 3);
+            const bool s = (now.half[kt].page >= 0) & (key <= row_pos) & ((key > row_pos - window) | (key < a.sinks));
+            sc[kt][r] = s ? sc[kt][r] : -INFINITY;
+          }
+      }
+      // ---- online softmax: a row is in the lanes l, l + 32 ----
+      if (kE4m3) {
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) sc[kt][r] *= now.half[kt].ks;
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[kt][r]);
+      mx = other_half_max(mx);
+      const float m_new = fmaxf(m_run, mx * a.scale);
+      if (__builtin_amdgcn_ballot_w64(m_new > m_run) != 0) {        // some row's maximum moved
+        const float keep = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+        l_run *= keep;
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[i][r] *= keep;
+        m_run = m_new;
+      }
+      const float base = m_new == -INFINITY ? 0.f : m_new;          // nothing seen yet: all p are 0
+      float sum0 = 0.f, sum1 = 0.f;
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int j = 0; j < 8; j += 2) {
+            float p0 = __builtin_amdgcn_exp2f(fmaf(sc[kt][8 * s + j], a.scale, -base));
+            float p1 = __builtin_amdgcn_exp2f(fmaf(sc[kt][8 * s + j + 1], a.scale, -base));
+            sum0 += p0;
+            sum1 += p1;
+            if (kE4m3) {
+              p0 *= now.half[kt].vs;
+              p1 *= now.half[kt].vs;
+            }
+            const f32x2 pp = {p0, p1};
+            const bf16x2 pb = __builtin_convertvector(pp, bf16x2);
+            pf[kt][s][j] = pb[0];
+            pf[kt][s][j + 1] = pb[1];
+          }
+      l_run += sum0 + sum1;
+
+    }
+
+    // 0 * NaN is NaN.  In a tile that not every row of the workgroup sees all of, infinities and NaN among the values
+    // are added to the rows that see them (p > 0 times one is one) and leave the tile before the product.
+    const bool inside = ((now.half[0].page | now.half[1].page) >= 0) & (last <= wg_first) & ((first > wg_last - window) | (last < a.sinks));
+    if (!inside) {
+      constexpr int kQuarter = kTileBytes / 4;
+      char* vb = lds_v + kBuf * kTileBytes;
+      uint32_t bad = 0;
+#pragma unroll
+      for (int i = 0; i < kQuarter / 1024; ++i) {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(vb + wave * kQuarter + i * 1024 + lane * 16);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) bad |= special_bits<false>(w[e]);
+      }
+      const bool some = __builtin_amdgcn_ballot_w64(bad != 0) != 0;
+      if (lane == 0) s_special[kBuf][wave] = some;
+      tile_barrier();
+      const int special = uniform(s_special[kBuf][0] | s_special[kBuf][1] | s_special[kBuf][2] | s_special[kBuf][3]);
+      if (special != 0) {
+        if (!none) {
+#pragma unroll 1
+          for (int j = 0; j < kChunkKeys; ++j) {
+            const int key = first + j;
+            const bool s = ((j < 32 ? now.half[0].page : now.half[1].page) >= 0) & (key <= row_pos) & ((key > row_pos - window) | (key < a.sinks));
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {               // dims dt * 32 + q * 8 + hf * 4 ..+3
+                const uint2 w = *reinterpret_cast<const uint2*>(vb + j * kRow + (((dt * 4 + q) ^ (v_row_swizzle<D>(j) << 2)) << 4) + hf * 8);
+                const float y[4] = {__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u), __uint_as_float(w.y << 16),
+                                    __uint_as_float(w.y & 0xFFFF0000u)};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[dt][4 * q + e] += s & !(fabsf(y[e]) < INFINITY) ? y[e] : 0.f;
+              }
+          }
+        }
+        tile_barrier();
+#pragma unroll
+        for (int i = 0; i < kQuarter / 1024; ++i) {
+          u32x4* w = reinterpret_cast<u32x4*>(vb + wave * kQuarter + i * 1024 + lane * 16);
+          *w = u32x4{without_specials<false>((*w)[0]), without_specials<false>((*w)[1]), without_specials<false>((*w)[2]), without_specials<false>((*w)[3])};
+        }
+        tile_barrier();
+      }
+    }
+
+    // ---- O^T += V^T P^T ----
+    if (!none) {
+      constexpr int kSteps = DT * KT * 2;
+      static_assert(kSteps >= kDepth, "pipeline deeper than the phase");
+      bf16x8 fr[kDepth];
+#pragma unroll
+      for (int i = 0; i < kDepth; ++i) fr[i] = v_frag(i % DT, i / DT, kBuf);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) {
+        const int dt = i % DT, st = i / DT;
+        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[i % kDepth], pf[st >> 1][st & 1], o[dt], 0, 0, 0);
+        if (i + kDepth < kSteps) fr[i % kDepth] = v_frag((i + kDepth) % DT, (i + kDepth) / DT, kBuf);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    if (kE4m3 && more) deliver(1 - kBuf);
+    wait_async_loads();                                   // this wave's share of the next tile has landed
+    tile_barrier();                                       // ... everyone's, and everyone is done with this one
+    now = next;
+  };
+
+  if (c0 < c1) {
+    now = locate(c0);
+    if (kE4m3) {
+      request();
+      deliver(0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) copy_k(i, 0);
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) copy_v(i, 0);
+    }
+    wait_async_loads();
+    tile_barrier();
+    int i = c0;
+    for (; i + 1 < c1; i += 2) {
+      step(std::integral_constant<int, 0>{}, i);
+      step(std::integral_constant<int, 1>{}, i + 1);
+    }
+    if (i < c1) step(std::integral_constant<int, 0>{}, i);
   }
-  if (t < D) {
-    const __bf16 y = (__bf16)(l == 0.f ? 0.f : o / l);
-    out.p[hq * out.head + token * out.token + t] = __builtin_bit_cast(uint16_t, y);
+
+  const float l = other_half_sum(l_run);
+  if (wave_row0 + l32 >= c.rows) return;
+  if (splits == 1) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    uint16_t* op = a.out.p + (int64_t)hq * a.out.head + (int64_t)(c.r.row0 + tok) * a.out.token;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<uint2*>(op + dt * 32 + q * 8 + hf * 4) =
+            make_uint2(bf16_pair(o[dt][4 * q] * inv, o[dt][4 * q + 1] * inv), bf16_pair(o[dt][4 * q + 2] * inv, o[dt][4 * q + 3] * inv));
+    if (a.lse != nullptr && hf == 0)
+      a.lse[(int64_t)hq * a.batch.n_tokens + c.r.row0 + tok] = l == 0.f ? -INFINITY : (m_run + log2f(l)) * kLn2;
+  } else {
+    const int64_t place = (((int64_t)kv * slots + at.slot) * splits + at.split) * kChunkRows + wave * 32 + l32;
+    float* pp = ws.part + place * D;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<float4*>(pp + dt * 32 + q * 8 + hf * 4) = make_float4(o[dt][4 * q], o[dt][4 * q + 1], o[dt][4 * q + 2], o[dt][4 * q + 3]);
+    if (hf == 0) ws.stats[place] = make_float2(m_run, l);
   }
-  if (t == 0 && lse != nullptr) lse[(int64_t)hq * batch.n_tokens + token] = l == 0.f ? -INFINITY : m + logf(l);
+#endif
+}
+
+// Joins the parts of the rows: one workgroup for kChunkThreads * 4 / D rows.
+template <int D>
+__global__ __launch_bounds__(kChunkThreads) void chunk_combine_kernel(AttnCall a, ChunkWs ws, int slots, int splits) {
+  constexpr int kRows = kChunkThreads * 4 / D;
+  const int slot = blockIdx.x, kv = blockIdx.y;
+  const ChunkRows c = chunk_rows(a, slot);
+  const int x = blockIdx.z * kRows + threadIdx.x / (D / 4), d0 = threadIdx.x % (D / 4) * 4, row = c.row0 + x;
+  if (row >= c.rows) return;
+  const int64_t place = ((int64_t)kv * slots + slot) * splits * kChunkRows + x;
+  float top = -INFINITY;
+  for (int i = 0; i < splits; ++i) top = fmaxf(top, ws.stats[place + (int64_t)i * kChunkRows].x);
+  const float base = top == -INFINITY ? 0.f : top;
+  float sum = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int i = 0; i < splits; ++i) {
+    const float2 st = ws.stats[place + (int64_t)i * kChunkRows];
+    const float4 y = *reinterpret_cast<const float4*>(ws.part + (place + (int64_t)i * kChunkRows) * D + d0);
+    const float f = __builtin_amdgcn_exp2f(st.x - base);
+    sum += f * st.y;
+    acc.x += f * y.x; acc.y += f * y.y; acc.z += f * y.z; acc.w += f * y.w;
+  }
+  const int tok = row / a.g, hq = kv * a.g + row - tok * a.g;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  *reinterpret_cast<uint2*>(a.out.p + (int64_t)hq * a.out.head + (int64_t)(c.r.row0 + tok) * a.out.token + d0) =
+      make_uint2(bf16_pair(acc.x * inv, acc.y * inv), bf16_pair(acc.z * inv, acc.w * inv));
+  if (a.lse != nullptr && d0 == 0)
+    a.lse[(int64_t)hq * a.batch.n_tokens + c.r.row0 + tok] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
 }
 
 // =====================================================================================
@@ -661,22 +1073,46 @@ __global__ __launch_bounds__(256) void cache_attn_simple_kernel(Rows q, Rows out
 constexpr int kWorkers = 512;                             // two workgroups a CU
 
 struct AttnPlan {
-  int mt;                  // 16-row tiles of the step kernel; 0: too many rows for it
-  int workers;
-  size_t part_bytes, bytes;
+  int step_rows;           // see AttnCall
+  int mt, workers;         // steps: 16-row tiles, workgroups (0: none of the call's sequences is one)
+  int slots, splits;       // chunks: row tiles of a kv head, parts of each (0: none)
+  size_t part_bytes, chunk_part_bytes, steps_bytes, bytes;
 };
+// Which kernels a call needs.  Up to 32 rows (16 at d = 256, where two row tiles do not fit the registers) a sequence and kv
+// head is a step's.  The lengths of a ragged batch are on the device: if its longest sequence has more rows, both kernels are
+// launched, and each leaves the other's sequences; steps are then those of one row tile.
 static AttnPlan plan_of(const prism_cache* c, const prism_batch* b, int n_q_heads) {
   AttnPlan p = {};
-  const int64_t rows = (int64_t)b->max_tokens * (n_q_heads / c->n_kv_heads);
-  p.mt = rows <= 16 ? 1 : (rows <= 32 && c->head_dim < 256 ? 2 : 0);
+  const int g = n_q_heads / c->n_kv_heads;
+  const int64_t rows = (int64_t)b->max_tokens * g;
   p.bytes = 256;
-  if (p.mt == 0 || b->n_seqs == 0) return p;
-  const int64_t units = (int64_t)b->n_seqs * c->n_kv_heads * (((int64_t)b->max_pages * c->page + 127) / 128);
-  const int most = c->head_dim == 256 || p.mt > 1 ? kWorkers / 2 : kWorkers;
-  p.workers = units < most ? (int)units : most;
-  const size_t slots = 2 * (size_t)p.workers * 16 * p.mt;
-  p.part_bytes = align_up(slots * c->head_dim * sizeof(float), 256);
-  p.bytes = p.part_bytes + align_up(slots * sizeof(float2), 256);
+  if (b->n_seqs == 0 || b->n_tokens == 0) return p;
+  const bool steps_only = rows <= (c->head_dim == 256 ? 16 : 32);
+  const bool ragged = b->cu_tokens != nullptr && b->n_seqs > 1;
+  if (steps_only || (ragged && g <= 16)) {
+    p.mt = steps_only && rows > 16 ? 2 : 1;
+    p.step_rows = 16 * p.mt;
+    const int64_t units = (int64_t)b->n_seqs * c->n_kv_heads * (((int64_t)b->max_pages * c->page + 127) / 128);
+    const int most = c->head_dim == 256 || p.mt > 1 ? kWorkers / 2 : kWorkers;
+    p.workers = units < most ? (int)units : most;
+    const size_t slots = 2 * (size_t)p.workers * 16 * p.mt;
+    p.part_bytes = align_up(slots * c->head_dim * sizeof(float), 256);
+    p.steps_bytes = p.part_bytes + align_up(slots * sizeof(float2), 256);
+  }
+  if (!steps_only) {
+    p.slots = (int)(((int64_t)b->n_tokens * g) >> 7) + b->n_seqs;
+    // parts until the chip is full, each of four tiles of keys at least
+    const int64_t tiles = (int64_t)p.slots * c->n_kv_heads, most = ((int64_t)b->max_pages * c->page + 255) / 256;
+    int64_t n = (c->head_dim == 256 ? kWorkers / 2 : kWorkers) / tiles;
+    n = n < most ? n : most;
+    p.splits = n > 1 ? (int)n : 1;
+    if (p.splits > 1) {
+      const size_t parts = (size_t)tiles * p.splits * kChunkRows;
+      p.chunk_part_bytes = align_up(parts * c->head_dim * sizeof(float), 256);
+      p.bytes = p.chunk_part_bytes + align_up(parts * sizeof(float2), 256);
+    }
+  }
+  p.bytes += p.steps_bytes;
   return p;
 }
 
@@ -697,11 +1133,22 @@ static int launch_steps(const AttnCall& a, const AttnPlan& p, char* ws, hipStrea
 }
 template <int D, bool kE4m3>
 static int launch_attn(const AttnCall& a, const AttnPlan& p, char* ws, hipStream_t st) {
-  if (p.mt == 1) return launch_steps<D, kE4m3, 1>(a, p, ws, st);
-  if constexpr (D < 256)
-    if (p.mt == 2) return launch_steps<D, kE4m3, 2>(a, p, ws, st);
-  hipLaunchKernelGGL((cache_attn_simple_kernel<D, kE4m3>), dim3(a.batch.n_tokens, a.h), dim3(256), 0, st, a.q, a.out, a.lse, a.cache,
-                     a.batch, a.h, a.window, a.sinks, a.scale * kLn2);
+  if (p.workers > 0) {
+    int rc = PRISM_OK;
+    if constexpr (D < 256) {
+      rc = p.mt == 2 ? launch_steps<D, kE4m3, 2>(a, p, ws, st) : launch_steps<D, kE4m3, 1>(a, p, ws, st);
+    } else {
+      rc = launch_steps<D, kE4m3, 1>(a, p, ws, st);
+    }
+    if (rc != PRISM_OK || p.slots == 0) return rc;
+  }
+  char* cw = ws + p.steps_bytes;
+  const ChunkWs w = {reinterpret_cast<float*>(cw), reinterpret_cast<float2*>(cw + p.chunk_part_bytes)};
+  hipLaunchKernelGGL((chunk_kernel<D, kE4m3>), dim3(chunk_grid(a.cache.h_kv, p.slots, p.splits)), dim3(kChunkThreads), 0, st, a, w, p.slots,
+                     p.splits);
+  if (p.splits > 1)
+    hipLaunchKernelGGL((chunk_combine_kernel<D>), dim3(p.slots, a.cache.h_kv, kChunkRows * D / (kChunkThreads * 4)), dim3(kChunkThreads), 0, st, a,
+                       w, p.slots, p.splits);
   return launch_status();
 }
 template <int D>
@@ -737,7 +1184,7 @@ extern "C" int prism_cache_attn(const prism_cache* cache, const prism_batch* bat
   if (workspace == nullptr || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < plan.bytes) return PRISM_ERR_WORKSPACE;
   const float scale = params->scale > 0.f ? params->scale : 1.f / sqrtf((float)d);
   const AttnCall a = {rows_of(q), rows_of(out), lse, cache_view(cache), batch_view(batch), h, h / cache->n_kv_heads,
-                      params->window, params->sinks, scale * kLog2e};
+                      params->window, params->sinks, scale * kLog2e, plan.step_rows};
   const bool e4m3 = cache->dtype == PRISM_CACHE_E4M3;
   char* ws = static_cast<char*>(workspace);
   hipStream_t st = static_cast<hipStream_t>(stream);
