@@ -86,20 +86,18 @@ __device__ __forceinline__ KeyRange keys_of(const AttnCall& a, const SeqRows& r)
 }
 
 // Prefix sums over the units of all sequences, 256 at a time.
-__device__ __forceinline__ int step_units(const AttnCall& a, int s) {
-  if (s >= a.batch.n_seqs) return 0;
-  return (keys_of(a, seq_rows(a.batch, s)).count() + kStepWaves - 1) / kStepWaves;
-}
 struct StepScan {
   int before[kStepThreads + 1];      // units of the sequences in front, within these 256
   int part[kStepWaves];
+  SeqRows rows[kStepThreads];
 };
 // all threads; returns the units of sequences s0 .. s0 + 255
 __device__ __forceinline__ int scan_units(StepScan& m, const AttnCall& a, int s0) {
   const int t = threadIdx.x, wave = t >> 6;
-  const int mine = step_units(a, s0 + t);
-  const int upto = wave_scan_inclusive(mine);
+  const SeqRows r = s0 + t < a.batch.n_seqs ? seq_rows(a.batch, s0 + t) : SeqRows{0, 0, 0};
+  const int upto = wave_scan_inclusive((keys_of(a, r).count() + kStepWaves - 1) / kStepWaves);
   __syncthreads();
+  m.rows[t] = r;
   if ((t & 63) == 63) m.part[wave] = upto;
   __syncthreads();
   int base = 0;
@@ -186,10 +184,7 @@ __global__ __launch_bounds__(kStepThreads, D == 256 || MT > 1 ? 1 : 2) void step
       const int64_t seq_first = chunk0 + (int64_t)before * h_kv;
       const int64_t seq_end = seq_first + (int64_t)units * h_kv;
       const int s = s0 + i;
-      SeqRows r = seq_rows(a.batch, s);
-      r.row0 = uniform(r.row0);
-      r.n = uniform(r.n);
-      r.length = uniform(r.length);
+      const SeqRows r = {uniform(scan.rows[i].row0), uniform(scan.rows[i].n), uniform(scan.rows[i].length)};
       const KeyRange keys = keys_of(a, r);
       const int n = min(r.n, a.batch.each), R = n * a.g;
       const int pos0 = r.length - r.n, pos_last = pos0 + n - 1;
@@ -512,15 +507,19 @@ __global__ __launch_bounds__(kStepThreads, D == 256 || MT > 1 ? 1 : 2) void step
 #endif
 }
 
-// Joins the parts of a (sequence, kv head) that several workgroups of step_kernel worked on, and writes the rows of
-// sequences in which no row sees anything.
+// Joins the parts of a row that several workgroups of step_kernel worked on, and writes the rows of sequences in which no row
+// sees anything.  One workgroup a row; kGroups groups of threads take every kGroups-th part, each with a maximum of its own, so
+// that all parts are requested at once.
 template <int D, int MT>
 __global__ __launch_bounds__(kStepThreads) void combine_kernel(AttnCall a, StepWs ws, int workgroups) {
-  constexpr int kGroups = kStepThreads * 4 / D;           // of threads, each with every kGroups-th part
+  constexpr int kGroups = kStepThreads * 4 / D;
   __shared__ StepScan scan;
   __shared__ float s_acc[kGroups][D];
-  __shared__ float s_sum[kGroups];
-  const int s = blockIdx.x, kv = blockIdx.y, t = threadIdx.x, h_kv = a.cache.h_kv;
+  __shared__ float s_top[kGroups], s_sum[kGroups];
+  const int s = blockIdx.x, kv = blockIdx.y, row = blockIdx.z, t = threadIdx.x, h_kv = a.cache.h_kv;
+  const SeqRows r = seq_rows(a.batch, s);
+  const int64_t rows = (int64_t)min(r.n, a.batch.each) * a.g;
+  if (row >= rows || rows > a.step_rows) return;
   int64_t total = 0, first = 0;
   int units = 0;
   for (int s0 = 0; s0 < a.batch.n_seqs; s0 += kStepThreads) {
@@ -533,56 +532,71 @@ __global__ __launch_bounds__(kStepThreads) void combine_kernel(AttnCall a, StepW
   }
   total *= h_kv;
   const int64_t W = shares(total, workgroups);
-  const SeqRows r = seq_rows(a.batch, s);
-  const int64_t rows = (int64_t)min(r.n, a.batch.each) * a.g;
-  const int R = rows > a.step_rows ? 0 : (int)rows;
   // the workgroup of unit x: the largest w with w * total / W <= x
   const int w0 = units > 0 ? (int)(((first + 1) * W - 1) / total) : 0;
   const int w1 = units > 0 ? (int)(((first + units) * W - 1) / total) : 0;
   if (units > 0 && w0 == w1) return;
   const int group = t / (D / 4), d0 = t % (D / 4) * 4;
-  for (int row = 0; row < R; ++row) {
-    float top = -INFINITY;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float sum = 0.f;
-    if (units > 0) {
-      for (int w = w0 + t; w <= w1; w += kStepThreads) top = fmaxf(top, ws.stats[(int64_t)(2 * w + (w == w0 ? 1 : 0)) * (16 * MT) + row].x);
-      top = wave_max(top);
-      __syncthreads();
-      if ((t & 63) == 0) s_acc[0][t >> 6] = top;
-      __syncthreads();
-      top = fmaxf(fmaxf(s_acc[0][0], s_acc[0][1]), fmaxf(s_acc[0][2], s_acc[0][3]));
-      const float base = top == -INFINITY ? 0.f : top;
-      for (int w = w0 + group; w <= w1; w += kGroups) {
-        const int64_t at = (int64_t)(2 * w + (w == w0 ? 1 : 0)) * (16 * MT) + row;
-        const float2 st = ws.stats[at];
-        const float4 x = *reinterpret_cast<const float4*>(ws.part + at * D + d0);
-        const float f = __builtin_amdgcn_exp2f(st.x - base);
-        sum += f * st.y;
-        acc.x += f * x.x; acc.y += f * x.y; acc.z += f * x.z; acc.w += f * x.w;
-      }
-      __syncthreads();
-      *reinterpret_cast<float4*>(&s_acc[group][d0]) = acc;
-      if (d0 == 0) s_sum[group] = sum;
-      __syncthreads();
-    }
-    if (group == 0) {
-      if (units > 0) {
+  float top = -INFINITY, sum = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (units > 0) {
+    constexpr int kAtOnce = 4;
+    for (int w = w0 + group; w <= w1; w += kAtOnce * kGroups) {
+      float2 st[kAtOnce];
+      float4 x[kAtOnce];
 #pragma unroll
-        for (int x = 1; x < kGroups; ++x) {
-          const float4 y = *reinterpret_cast<const float4*>(&s_acc[x][d0]);
-          acc.x += y.x; acc.y += y.y; acc.z += y.z; acc.w += y.w;
-          sum += s_sum[x];
+      for (int i = 0; i < kAtOnce; ++i) {
+        const int wi = w + i * kGroups;
+        st[i] = make_float2(-INFINITY, 0.f);
+        x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (wi <= w1) {
+          const int64_t at = (int64_t)(2 * wi + (wi == w0 ? 1 : 0)) * (16 * MT) + row;
+          st[i] = ws.stats[at];
+          x[i] = *reinterpret_cast<const float4*>(ws.part + at * D + d0);
         }
       }
-      const int tok = row / a.g, hq = kv * a.g + row - tok * a.g;
-      const float inv = sum == 0.f ? 0.f : 1.f / sum;
-      *reinterpret_cast<uint2*>(a.out.p + (int64_t)hq * a.out.head + (int64_t)(r.row0 + tok) * a.out.token + d0) =
-          make_uint2(bf16_pair(acc.x * inv, acc.y * inv), bf16_pair(acc.z * inv, acc.w * inv));
-      if (a.lse != nullptr && d0 == 0)
-        a.lse[(int64_t)hq * a.batch.n_tokens + r.row0 + tok] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+      float m = top;
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) m = fmaxf(m, st[i].x);
+      const float base = m == -INFINITY ? 0.f : m, keep = __builtin_amdgcn_exp2f(top - base);
+      top = m;
+      sum *= keep;
+      acc.x *= keep; acc.y *= keep; acc.z *= keep; acc.w *= keep;
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const float f = __builtin_amdgcn_exp2f(st[i].x - base);
+        sum += f * st[i].y;
+        acc.x += f * x[i].x; acc.y += f * x[i].y; acc.z += f * x[i].z; acc.w += f * x[i].w;
+      }
+    }
+    *reinterpret_cast<float4*>(&s_acc[group][d0]) = acc;
+    if (d0 == 0) {
+      s_top[group] = top;
+      s_sum[group] = sum;
+    }
+    __syncthreads();
+  }
+  if (group != 0) return;
+  if (units > 0) {
+#pragma unroll
+    for (int x = 1; x < kGroups; ++x) top = fmaxf(top, s_top[x]);
+    const float base = top == -INFINITY ? 0.f : top;
+    sum = 0.f;
+    acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int x = 0; x < kGroups; ++x) {
+      const float4 y = *reinterpret_cast<const float4*>(&s_acc[x][d0]);
+      const float f = __builtin_amdgcn_exp2f(s_top[x] - base);
+      sum += f * s_sum[x];
+      acc.x += f * y.x; acc.y += f * y.y; acc.z += f * y.z; acc.w += f * y.w;
     }
   }
+  const int tok = row / a.g, hq = kv * a.g + row - tok * a.g;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  *reinterpret_cast<uint2*>(a.out.p + (int64_t)hq * a.out.head + (int64_t)(r.row0 + tok) * a.out.token + d0) =
+      make_uint2(bf16_pair(acc.x * inv, acc.y * inv), bf16_pair(acc.z * inv, acc.w * inv));
+  if (a.lse != nullptr && d0 == 0)
+    a.lse[(int64_t)hq * a.batch.n_tokens + r.row0 + tok] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
 }
 
 // =====================================================================================
@@ -1074,7 +1088,7 @@ constexpr int kWorkers = 512;                             // two workgroups a CU
 
 struct AttnPlan {
   int step_rows;           // see AttnCall
-  int mt, workers;         // steps: 16-row tiles, workgroups (0: none of the call's sequences is one)
+  int mt, workers, rows;   // steps: 16-row tiles, workgroups (0: none of the call's sequences is one), rows of a kv head at most
   int slots, splits;       // chunks: row tiles of a kv head, parts of each (0: none)
   size_t part_bytes, chunk_part_bytes, steps_bytes, bytes;
 };
@@ -1092,6 +1106,7 @@ static AttnPlan plan_of(const prism_cache* c, const prism_batch* b, int n_q_head
   if (steps_only || (ragged && g <= 16)) {
     p.mt = steps_only && rows > 16 ? 2 : 1;
     p.step_rows = 16 * p.mt;
+    p.rows = (int)(rows < p.step_rows ? rows : p.step_rows);
     const int64_t units = (int64_t)b->n_seqs * c->n_kv_heads * (((int64_t)b->max_pages * c->page + 127) / 128);
     const int most = c->head_dim == 256 || p.mt > 1 ? kWorkers / 2 : kWorkers;
     p.workers = units < most ? (int)units : most;
@@ -1128,7 +1143,7 @@ template <int D, bool kE4m3, int MT>
 static int launch_steps(const AttnCall& a, const AttnPlan& p, char* ws, hipStream_t st) {
   const StepWs w = {reinterpret_cast<float*>(ws), reinterpret_cast<float2*>(ws + p.part_bytes)};
   hipLaunchKernelGGL((step_kernel<D, kE4m3, MT>), dim3(p.workers), dim3(kStepThreads), 0, st, a, w);
-  hipLaunchKernelGGL((combine_kernel<D, MT>), dim3(a.batch.n_seqs, a.cache.h_kv), dim3(kStepThreads), 0, st, a, w, p.workers);
+  hipLaunchKernelGGL((combine_kernel<D, MT>), dim3(a.batch.n_seqs, a.cache.h_kv, p.rows), dim3(kStepThreads), 0, st, a, w, p.workers);
   return launch_status();
 }
 template <int D, bool kE4m3>
