@@ -725,6 +725,8 @@ __global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(
   const int32_t* table = a.batch.table + (int64_t)c.s * a.batch.max_pages;
   int held_from = -64, held = 0;
   float held_ks = 0.f, held_vs = 0.f;
+  // e4m3: the values' scale is a power of two, which the conversion to bf16 applies, times vs in [1, 2): 1 for scales of
+  // prism_cache_append, and the probabilities need no factor
   struct Half {
     int page;                                             // < 0: none
     float ks, vs;
@@ -737,6 +739,7 @@ __global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(
   TileRsrc krs[2], vrs[2];
   const char *k_at[2], *v_at[2];
   int half_bytes[2];
+  float v_power[2];
   auto locate = [&](int list_at) __attribute__((always_inline)) {
     Tile x;
     x.first = keys.tile(list_at) * kChunkKeys;
@@ -758,7 +761,9 @@ __global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(
       y.page = __builtin_amdgcn_readlane(held, e - held_from);
       if (kE4m3) {
         y.ks = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, held_ks), e - held_from));
-        y.vs = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, held_vs), e - held_from));
+        const int vs = __builtin_amdgcn_readlane(__builtin_bit_cast(int, held_vs), e - held_from);
+        y.vs = __builtin_bit_cast(float, (vs & 0x007FFFFF) | 0x3F800000);
+        v_power[hv] = __builtin_bit_cast(float, vs & 0x7F800000);
       }
       constexpr int kPageRow = kE4m3 ? D : kRow;
       const int64_t off = max(y.page, 0) * a.cache.page_stride + (int64_t)(kv * a.cache.page + (tk & (a.cache.page - 1))) * kPageRow;
@@ -806,11 +811,12 @@ __global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(
 #pragma unroll
       for (int hv = 0; hv < 2; ++hv) {
         u32x4 kw, vw;
+        const float power = (kWideRp == 64 ? uniform(r >> 5) : i * kWideRp / 32) ? v_power[1] : v_power[0];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const uint32_t k8 = kx[i][2 * hv + (e >> 1)], v8 = vx[i][2 * hv + (e >> 1)];
           kw[e] = __builtin_bit_cast(uint32_t, (e & 1) ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(k8, 1.0f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(k8, 1.0f, false));
-          vw[e] = __builtin_bit_cast(uint32_t, (e & 1) ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v8, 1.0f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v8, 1.0f, false));
+          vw[e] = __builtin_bit_cast(uint32_t, (e & 1) ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v8, power, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v8, power, false));
         }
         *reinterpret_cast<u32x4*>(lds_k + b * kTileBytes + r * kRow + (((ch + hv) ^ k_row_swizzle<D>(r)) << 4)) = kw;
         *reinterpret_cast<u32x4*>(lds_v + b * kTileBytes + r * kRow + (((ch + hv) ^ (v_row_swizzle<D>(r) << 2)) << 4)) = vw;
@@ -843,7 +849,7 @@ __global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(
     const int first = now.first, last = first + kChunkKeys - 1;
     const bool none = idle || first > pos_last || (last <= pos_first - window && first >= a.sinks);
     bf16x8 pf[KT][2];
-    constexpr int kDepth = 8;
+    constexpr int kDepth = 6;
     if (none) {
       if (!kE4m3 && more) {
 #pragma unroll
@@ -864,6 +870,7 @@ __global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
           const int kt = i % KT, ks = i / KT;
+          if (i == 0) __builtin_amdgcn_s_setprio(1);
           sc[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[i % kDepth], qf[ks], ks == 0 ? zero16 : sc[kt], 0, 0, 0);
           if (i + kDepth < kSteps) {
             const int j = i + kDepth;
@@ -878,6 +885,7 @@ __global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(
           __builtin_amdgcn_sched_barrier(0);
         }
       }
+      __builtin_amdgcn_s_setprio(0);
       // ---- what a row sees: all of the tile, or each key for itself (without branches, as in step_kernel) ----
       const bool whole = ((now.half[0].page | now.half[1].page) >= 0) & (last <= pos_first) & ((first > pos_last - window) | (last < a.sinks));
       if (!whole) {
@@ -891,19 +899,16 @@ __global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(
           }
       }
       // ---- online softmax: a row is in the lanes l, l + 32 ----
-      if (kE4m3) {
+      float by[KT], mx = -INFINITY;
 #pragma unroll
-        for (int kt = 0; kt < KT; ++kt)
+      for (int kt = 0; kt < KT; ++kt) {
+        by[kt] = kE4m3 ? a.scale * now.half[kt].ks : a.scale;
+        float y = sc[kt][0];
 #pragma unroll
-          for (int r = 0; r < 16; ++r) sc[kt][r] *= now.half[kt].ks;
+        for (int r = 1; r < 16; ++r) y = fmaxf(y, sc[kt][r]);
+        mx = fmaxf(mx, y * by[kt]);
       }
-      float mx = -INFINITY;
-#pragma unroll
-      for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[kt][r]);
-      mx = other_half_max(mx);
-      const float m_new = fmaxf(m_run, mx * a.scale);
+      const float m_new = fmaxf(m_run, other_half_max(mx));
       if (__builtin_amdgcn_ballot_w64(m_new > m_run) != 0) {        // some row's maximum moved
         const float keep = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
         l_run *= keep;
@@ -915,25 +920,29 @@ __global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(
       }
       const float base = m_new == -INFINITY ? 0.f : m_new;          // nothing seen yet: all p are 0
       float sum0 = 0.f, sum1 = 0.f;
+      auto probabilities = [&](auto scaled) __attribute__((always_inline)) {
 #pragma unroll
-      for (int kt = 0; kt < KT; ++kt)
+        for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-          for (int j = 0; j < 8; j += 2) {
-            float p0 = __builtin_amdgcn_exp2f(fmaf(sc[kt][8 * s + j], a.scale, -base));
-            float p1 = __builtin_amdgcn_exp2f(fmaf(sc[kt][8 * s + j + 1], a.scale, -base));
+          for (int r = 0; r < 16; r += 2) {
+            float p0 = __builtin_amdgcn_exp2f(fmaf(sc[kt][r], by[kt], -base));
+            float p1 = __builtin_amdgcn_exp2f(fmaf(sc[kt][r + 1], by[kt], -base));
             sum0 += p0;
             sum1 += p1;
-            if (kE4m3) {
+            if (decltype(scaled)::value) {
               p0 *= now.half[kt].vs;
               p1 *= now.half[kt].vs;
             }
             const f32x2 pp = {p0, p1};
             const bf16x2 pb = __builtin_convertvector(pp, bf16x2);
-            pf[kt][s][j] = pb[0];
-            pf[kt][s][j + 1] = pb[1];
+            pf[kt][r >> 3][r & 7] = pb[0];
+            pf[kt][r >> 3][(r & 7) + 1] = pb[1];
           }
+      };
+      if (kE4m3 && (now.half[0].vs != 1.f || now.half[1].vs != 1.f))
+        probabilities(std::true_type{});
+      else
+        probabilities(std::false_type{});
       l_run += sum0 + sum1;
 
     }
@@ -985,6 +994,7 @@ __global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(
 
     // ---- O^T += V^T P^T ----
     if (!none) {
+      __builtin_amdgcn_s_setprio(1);
       constexpr int kSteps = DT * KT * 2;
       static_assert(kSteps >= kDepth, "pipeline deeper than the phase");
       bf16x8 fr[kDepth];
@@ -999,6 +1009,7 @@ __global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(
         __builtin_amdgcn_sched_barrier(0);
       }
     }
+    __builtin_amdgcn_s_setprio(0);
     if (kE4m3 && more) deliver(1 - kBuf);
     wait_async_loads();                                   // this wave's share of the next tile has landed
     tile_barrier();                                       // ... everyone's, and everyone is done with this one
