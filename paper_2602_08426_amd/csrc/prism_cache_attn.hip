@@ -27,6 +27,14 @@ __device__ __forceinline__ uint32_t without_specials(uint32_t w) {
   return w & ~(kE4m3 ? (n >> 7) * 0xFFu : (n >> 15) * 0xFFFFu);
 }
 
+// eight e4m3 values times a power of two as bf16
+__device__ __forceinline__ u32x4 bf16_of_e4m3(uint32_t lo, uint32_t hi, float power) {
+  return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, power, false)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, power, true)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, power, false)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, power, true))};
+}
+
 // What the kernels need to know of a call.
 struct AttnCall {
   Rows q, out;
@@ -726,20 +734,16 @@ __global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(
   int held_from = -64, held = 0;
   float held_ks = 0.f, held_vs = 0.f;
   // e4m3: the values' scale is a power of two, which the conversion to bf16 applies, times vs in [1, 2): 1 for scales of
-  // prism_cache_append, and the probabilities need no factor
+  // prism_cache_append, and the probabilities need no factor.
   struct Half {
-    int page;                                             // < 0: none
-    float ks, vs;
+    int page, bytes;                                      // page < 0: none; bytes that are there: what lies behind reads as zero
+    int64_t off;                                          // in K and in V
+    float ks, vs, v_power;
   };
   struct Tile {
     int first;                                            // its first key
     Half half[2];
   };
-  // halves of the tile that is being requested
-  TileRsrc krs[2], vrs[2];
-  const char *k_at[2], *v_at[2];
-  int half_bytes[2];
-  float v_power[2];
   auto locate = [&](int list_at) __attribute__((always_inline)) {
     Tile x;
     x.first = keys.tile(list_at) * kChunkKeys;
@@ -763,64 +767,57 @@ __global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(
         y.ks = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, held_ks), e - held_from));
         const int vs = __builtin_amdgcn_readlane(__builtin_bit_cast(int, held_vs), e - held_from);
         y.vs = __builtin_bit_cast(float, (vs & 0x007FFFFF) | 0x3F800000);
-        v_power[hv] = __builtin_bit_cast(float, vs & 0x7F800000);
+        y.v_power = __builtin_bit_cast(float, vs & 0x7F800000);
       }
       constexpr int kPageRow = kE4m3 ? D : kRow;
-      const int64_t off = max(y.page, 0) * a.cache.page_stride + (int64_t)(kv * a.cache.page + (tk & (a.cache.page - 1))) * kPageRow;
-      // what lies behind the last token, or in no page, reads as zero
-      const int bytes = y.page < 0 ? 0 : max(min(32, c.r.length - tk), 0) * kPageRow;
-      if constexpr (kE4m3) {
-        k_at[hv] = a.cache.k + off;
-        v_at[hv] = a.cache.v + off;
-        half_bytes[hv] = bytes;
-      } else {
-        krs[hv] = make_tile_rsrc(a.cache.k + off, bytes);
-        vrs[hv] = make_tile_rsrc(a.cache.v + off, bytes);
-      }
+      y.off = max(y.page, 0) * a.cache.page_stride + (int64_t)(kv * a.cache.page + (tk & (a.cache.page - 1))) * kPageRow;
+      y.bytes = y.page < 0 ? 0 : max(min(32, c.r.length - tk), 0) * kPageRow;
     }
     return x;
   };
-  const int wave_base = t & ~63;
-  // piece i of the tile in krs / vrs, to buffer b
-  auto copy_k = [&](int i, int b) __attribute__((always_inline)) {
-    const int j = i % kHalf;
-    async_piece(krs[i / kHalf], k_lane[j & 1], (j & 2) * kRp * kRow, (uint32_t)(size_t)lds_k + b * kTileBytes + (i * kChunkThreads + uniform(wave_base)) * 16);
+  const int wave_base = uniform(t & ~63);
+  // piece i of K or V of a tile (its halves' resources), to buffer b
+  auto resources = [&](TileRsrc(&rs)[2], const char* base, const Tile& x) __attribute__((always_inline)) {
+#pragma unroll
+    for (int hv = 0; hv < 2; ++hv) rs[hv] = make_tile_rsrc(base + x.half[hv].off, x.half[hv].bytes);
   };
-  auto copy_v = [&](int i, int b) __attribute__((always_inline)) {
+  auto copy_k = [&](const TileRsrc(&rs)[2], int i, int b) __attribute__((always_inline)) {
     const int j = i % kHalf;
-    async_piece(vrs[i / kHalf], v_lane[j & 1], (j & 2) * kRp * kRow, (uint32_t)(size_t)lds_v + b * kTileBytes + (i * kChunkThreads + uniform(wave_base)) * 16);
+    async_piece(rs[i / kHalf], k_lane[j & 1], (j & 2) * kRp * kRow, (uint32_t)(size_t)lds_k + b * kTileBytes + (i * kChunkThreads + wave_base) * 16);
+  };
+  auto copy_v = [&](const TileRsrc(&rs)[2], int i, int b) __attribute__((always_inline)) {
+    const int j = i % kHalf;
+    async_piece(rs[i / kHalf], v_lane[j & 1], (j & 2) * kRp * kRow, (uint32_t)(size_t)lds_v + b * kTileBytes + (i * kChunkThreads + wave_base) * 16);
   };
   // e4m3: 16 values a piece, through registers
   u32x4 kx[kWide > 0 ? kWide : 1], vx[kWide > 0 ? kWide : 1];
   constexpr int kWideCpr = D / 16, kWideRp = kChunkThreads / kWideCpr;    // rows of a piece of all threads: 64, 32, 16
-  auto request = [&]() __attribute__((always_inline)) {
+  auto wide_half = [&](int i) __attribute__((always_inline)) { return kWideRp == 64 ? uniform(t / kWideCpr >> 5) : i * kWideRp / 32; };
+  auto request = [&](u32x4(&to)[kWide > 0 ? kWide : 1], const char* base, const Tile& x) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < kWide; ++i) {
-      const int r = i * kWideRp + t / kWideCpr;           // of the tile
-      const int hv = kWideRp == 64 ? uniform(r >> 5) : i * kWideRp / 32;
-      const int off = (r & 31) * D + (t % kWideCpr) * 16;
-      const int bytes = hv ? half_bytes[1] : half_bytes[0];
-      kx[i] = __builtin_amdgcn_raw_buffer_load_b128(make_rsrc(hv ? k_at[1] : k_at[0], bytes), off, 0, 0);
-      vx[i] = __builtin_amdgcn_raw_buffer_load_b128(make_rsrc(hv ? v_at[1] : v_at[0], bytes), off, 0, 0);
+      const int r = i * kWideRp + t / kWideCpr, hv = wide_half(i);
+      to[i] = __builtin_amdgcn_raw_buffer_load_b128(make_rsrc(base + (hv ? x.half[1].off : x.half[0].off), hv ? x.half[1].bytes : x.half[0].bytes),
+                                                    (r & 31) * D + (t % kWideCpr) * 16, 0, 0);
     }
   };
-  auto deliver = [&](int b) __attribute__((always_inline)) {
+  auto deliver_k = [&](int b) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < kWide; ++i) {
       const int r = i * kWideRp + t / kWideCpr, ch = 2 * (t % kWideCpr);
 #pragma unroll
-      for (int hv = 0; hv < 2; ++hv) {
-        u32x4 kw, vw;
-        const float power = (kWideRp == 64 ? uniform(r >> 5) : i * kWideRp / 32) ? v_power[1] : v_power[0];
+      for (int hv = 0; hv < 2; ++hv)
+        *reinterpret_cast<u32x4*>(lds_k + b * kTileBytes + r * kRow + (((ch + hv) ^ k_row_swizzle<D>(r)) << 4)) = bf16_of_e4m3(kx[i][2 * hv], kx[i][2 * hv + 1], 1.f);
+    }
+  };
+  auto deliver_v = [&](int b, const Tile& x) __attribute__((always_inline)) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t k8 = kx[i][2 * hv + (e >> 1)], v8 = vx[i][2 * hv + (e >> 1)];
-          kw[e] = __builtin_bit_cast(uint32_t, (e & 1) ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(k8, 1.0f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(k8, 1.0f, false));
-          vw[e] = __builtin_bit_cast(uint32_t, (e & 1) ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v8, power, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v8, power, false));
-        }
-        *reinterpret_cast<u32x4*>(lds_k + b * kTileBytes + r * kRow + (((ch + hv) ^ k_row_swizzle<D>(r)) << 4)) = kw;
-        *reinterpret_cast<u32x4*>(lds_v + b * kTileBytes + r * kRow + (((ch + hv) ^ (v_row_swizzle<D>(r) << 2)) << 4)) = vw;
-      }
+    for (int i = 0; i < kWide; ++i) {
+      const int r = i * kWideRp + t / kWideCpr, ch = 2 * (t % kWideCpr);
+      const float power = wide_half(i) ? x.half[1].v_power : x.half[0].v_power;
+#pragma unroll
+      for (int hv = 0; hv < 2; ++hv)
+        *reinterpret_cast<u32x4*>(lds_v + b * kTileBytes + r * kRow + (((ch + hv) ^ (v_row_swizzle<D>(r) << 2)) << 4)) = bf16_of_e4m3(vx[i][2 * hv], vx[i][2 * hv + 1], power);
     }
   };
   // A operand of O^T: dims 32*dt .. +31, keys 16*st + 8*(j/4) + 4*hf + j%4
@@ -838,119 +835,138 @@ __global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(
     for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
   float m_run = -INFINITY, l_run = 0.f;
   const int window = a.window > 0 ? a.window : 0x40000000;
+  constexpr int kDepth = 3;                               // LDS reads ahead of their MFMA
+  const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 
-  Tile now = {}, next = {};
-  // tile `now` in buffer kBuf; with `more` the tile in `next`, located here, goes to the other one
-  auto step = [&](auto buf_tag, int list_at) __attribute__((always_inline)) {
-    constexpr int kBuf = decltype(buf_tag)::value;
-    const bool more = list_at + 1 < c1;
-    if (more) next = locate(list_at + 1);
-    if (kE4m3 && more) request();
-    const int first = now.first, last = first + kChunkKeys - 1;
-    const bool none = idle || first > pos_last || (last <= pos_first - window && first >= a.sinks);
-    bf16x8 pf[KT][2];
-    constexpr int kDepth = 6;
-    if (none) {
-      if (!kE4m3 && more) {
+  // S^T of a tile whose K is in buffer kBuf, with `between(i)` behind MFMA i
+  auto scores = [&](f32x16(&sc)[KT], auto buf_tag, auto between) __attribute__((always_inline)) {
+    constexpr int kBuf = decltype(buf_tag)::value, kSteps = KT * KS;
+    static_assert(kSteps >= kDepth, "pipeline deeper than the phase");
+    const char* kb = lds_k + kBuf * kTileBytes;
+    bf16x8 fr[kDepth];
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) copy_k(i, 1 - kBuf);
+    for (int i = 0; i < kDepth; ++i) fr[i] = *reinterpret_cast<const bf16x8*>(kb + (i % KT) * kSlab + koff[i / KT]);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) copy_v(i, 1 - kBuf);
+    for (int i = 0; i < kSteps; ++i) {
+      const int kt = i % KT, ks = i / KT, j = i + kDepth;
+      sc[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[i % kDepth], qf[ks], ks == 0 ? zero16 : sc[kt], 0, 0, 0);
+      if (j < kSteps) fr[i % kDepth] = *reinterpret_cast<const bf16x8*>(kb + (j % KT) * kSlab + koff[j / KT]);
+      between(i);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  // whether all rows of the workgroup see all of a tile
+  auto inside = [&](const Tile& x) __attribute__((always_inline)) {
+    return ((x.half[0].page | x.half[1].page) >= 0) & (x.first + kChunkKeys - 1 <= wg_first) &
+           ((x.first > wg_last - window) | (x.first + kChunkKeys - 1 < a.sinks));
+  };
+  // scores of keys that a row does not see (without branches, as in step_kernel)
+  auto hide = [&](f32x16(&sc)[KT], const Tile& x) __attribute__((always_inline)) {
+    int pos = row_pos;
+    asm volatile("" : "+v"(pos));                         // formed here, not kept from in front of the loop
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int key = x.first + kt * 32 + 8 * (r >> 2) + 4 * hf + (r & 3);
+        const bool s = (x.half[kt].page >= 0) & (key <= pos) & ((key > pos - window) | (key < a.sinks));
+        sc[kt][r] = s ? sc[kt][r] : -INFINITY;
       }
-    } else {
-      f32x16 sc[KT];
-      {
+  };
+  // the running maximum (mx: this lane's of each 32 keys), and everything that was scaled by the one before
+  auto raise = [&](const float (&mx)[KT], const Tile& x) __attribute__((always_inline)) {
+    float y = -INFINITY;
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) y = fmaxf(y, mx[kt] * (kE4m3 ? a.scale * x.half[kt].ks : a.scale));
+    const float m_new = fmaxf(m_run, other_half_max(y));
+    if (__builtin_amdgcn_ballot_w64(m_new > m_run) != 0) {          // some row's maximum moved
+      const float keep = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+      l_run *= keep;
+#pragma unroll
+      for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[i][r] *= keep;
+      m_run = m_new;
+    }
+  };
+
+  bool specials = false;
+  Tile now = {}, next = {}, after = {};
+  f32x16 sa[KT], sb[KT];                                  // scores of this tile and of the next one, by turns
+  // Tile `now`, its scores in sc_now and below m_run; K of `next` and V of `now` are in LDS.
+  //   phase 1: S^T of the next tile, between its MFMAs the exponentials of this one and the requests of K two tiles and V one
+  //            tile ahead
+  //   phase 2: O^T += V^T P^T of this tile, between its MFMAs the maximum of the next one's scores
+  // A MFMA leaves its wave room for about five vector instructions; with scores, softmax and product one after the other the two
+  // waves of a SIMD did not fill each other's gaps (MFMAs and vector instructions together were 94 % of the time).
+  auto step = [&](auto buf_tag, auto last_tag, f32x16(&sc_now)[KT], f32x16(&sc_next)[KT], int list_at) __attribute__((always_inline)) {
+    constexpr int kBuf = decltype(buf_tag)::value;        // V of `now`, K of the tile two ahead
+    constexpr bool kLast = decltype(last_tag)::value;     // no next tile
+    const bool two = list_at + 2 < c1;
+    TileRsrc krs[2], vrs[2];
+    if (!kLast) {
+      if (two) after = locate(list_at + 2);
+      if (kE4m3) {
+        request(vx, a.cache.v, next);
+        if (two) request(kx, a.cache.k, after);
+      } else {
+        resources(vrs, a.cache.v, next);
+        resources(krs, a.cache.k, after);
+      }
+    }
+    const float base = m_run == -INFINITY ? 0.f : m_run;  // nothing seen yet: all p are 0
+    float by[KT];
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) by[kt] = kE4m3 ? a.scale * now.half[kt].ks : a.scale;
+    bf16x8 pf[KT][2];
+    float sum0 = 0.f, sum1 = 0.f;
+    auto phase1 = [&](auto scaled) __attribute__((always_inline)) {
+      auto pair = [&](int e) __attribute__((always_inline)) {       // scores 2e, 2e + 1 of this lane
+        const int kt = e >> 3, r = 2 * (e & 7);
+        float p0 = __builtin_amdgcn_exp2f(fmaf(sc_now[kt][r], by[kt], -base));
+        float p1 = __builtin_amdgcn_exp2f(fmaf(sc_now[kt][r + 1], by[kt], -base));
+        sum0 += p0;
+        sum1 += p1;
+        if (decltype(scaled)::value) {
+          p0 *= now.half[kt].vs;
+          p1 *= now.half[kt].vs;
+        }
+        const f32x2 pp = {p0, p1};
+        const bf16x2 pb = __builtin_convertvector(pp, bf16x2);
+        pf[kt][r >> 3][r & 7] = pb[0];
+        pf[kt][r >> 3][(r & 7) + 1] = pb[1];
+      };
+      constexpr int kPairs = 8 * KT;
+      if constexpr (kLast) {
+#pragma unroll
+        for (int e = 0; e < kPairs; ++e) pair(e);
+      } else {
         constexpr int kSteps = KT * KS, kEvery = kSteps / (2 * kPieces);
-        static_assert(kSteps >= kDepth && kSteps % (2 * kPieces) == 0, "pieces between the MFMAs");
-        const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        bf16x8 fr[kDepth];
-#pragma unroll
-        for (int i = 0; i < kDepth; ++i) fr[i] = *reinterpret_cast<const bf16x8*>(lds_k + kBuf * kTileBytes + (i % KT) * kSlab + koff[i / KT]);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-          const int kt = i % KT, ks = i / KT;
-          if (i == 0) __builtin_amdgcn_s_setprio(1);
-          sc[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[i % kDepth], qf[ks], ks == 0 ? zero16 : sc[kt], 0, 0, 0);
-          if (i + kDepth < kSteps) {
-            const int j = i + kDepth;
-            fr[i % kDepth] = *reinterpret_cast<const bf16x8*>(lds_k + kBuf * kTileBytes + (j % KT) * kSlab + koff[j / KT]);
-          }
+        static_assert(kSteps % (2 * kPieces) == 0, "pieces between the MFMAs");
+        scores(sc_next, std::integral_constant<int, 1 - kBuf>{}, [&](int i) __attribute__((always_inline)) {
           if (!kE4m3 && i % kEvery == 0) {
             const int p = i / kEvery;
-            if (more) {
-              if (p < kPieces) copy_k(p, 1 - kBuf); else copy_v(p - kPieces, 1 - kBuf);
-            }
+            if (p < kPieces) copy_v(vrs, p, 1 - kBuf);
+            else if (two) copy_k(krs, p - kPieces, kBuf);
           }
-          __builtin_amdgcn_sched_barrier(0);
-        }
+#pragma unroll
+          for (int e = i * kPairs / kSteps; e < (i + 1) * kPairs / kSteps; ++e) pair(e);
+        });
       }
-      __builtin_amdgcn_s_setprio(0);
-      // ---- what a row sees: all of the tile, or each key for itself (without branches, as in step_kernel) ----
-      const bool whole = ((now.half[0].page | now.half[1].page) >= 0) & (last <= pos_first) & ((first > pos_last - window) | (last < a.sinks));
-      if (!whole) {
-#pragma unroll
-        for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int key = first + kt * 32 + 8 * (r >> 2) + 4 * hf + (r & 3);
-            const bool s = (now.half[kt].page >= 0) & (key <= row_pos) & ((key > row_pos - window) | (key < a.sinks));
-            sc[kt][r] = s ? sc[kt][r] : -INFINITY;
-          }
-      }
-      // ---- online softmax: a row is in the lanes l, l + 32 ----
-      float by[KT], mx = -INFINITY;
-#pragma unroll
-      for (int kt = 0; kt < KT; ++kt) {
-        by[kt] = kE4m3 ? a.scale * now.half[kt].ks : a.scale;
-        float y = sc[kt][0];
-#pragma unroll
-        for (int r = 1; r < 16; ++r) y = fmaxf(y, sc[kt][r]);
-        mx = fmaxf(mx, y * by[kt]);
-      }
-      const float m_new = fmaxf(m_run, other_half_max(mx));
-      if (__builtin_amdgcn_ballot_w64(m_new > m_run) != 0) {        // some row's maximum moved
-        const float keep = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
-        l_run *= keep;
-#pragma unroll
-        for (int i = 0; i < DT; ++i)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) o[i][r] *= keep;
-        m_run = m_new;
-      }
-      const float base = m_new == -INFINITY ? 0.f : m_new;          // nothing seen yet: all p are 0
-      float sum0 = 0.f, sum1 = 0.f;
-      auto probabilities = [&](auto scaled) __attribute__((always_inline)) {
-#pragma unroll
-        for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-          for (int r = 0; r < 16; r += 2) {
-            float p0 = __builtin_amdgcn_exp2f(fmaf(sc[kt][r], by[kt], -base));
-            float p1 = __builtin_amdgcn_exp2f(fmaf(sc[kt][r + 1], by[kt], -base));
-            sum0 += p0;
-            sum1 += p1;
-            if (decltype(scaled)::value) {
-              p0 *= now.half[kt].vs;
-              p1 *= now.half[kt].vs;
-            }
-            const f32x2 pp = {p0, p1};
-            const bf16x2 pb = __builtin_convertvector(pp, bf16x2);
-            pf[kt][r >> 3][r & 7] = pb[0];
-            pf[kt][r >> 3][(r & 7) + 1] = pb[1];
-          }
-      };
-      if (kE4m3 && (now.half[0].vs != 1.f || now.half[1].vs != 1.f))
-        probabilities(std::true_type{});
-      else
-        probabilities(std::false_type{});
-      l_run += sum0 + sum1;
+    };
+    __builtin_amdgcn_s_setprio(1);
+    if (kE4m3 && (now.half[0].vs != 1.f || now.half[1].vs != 1.f))
+      phase1(std::true_type{});
+    else
+      phase1(std::false_type{});
+    __builtin_amdgcn_s_setprio(0);
+    l_run += sum0 + sum1;
 
-    }
-
-    // 0 * NaN is NaN.  In a tile that not every row of the workgroup sees all of, infinities and NaN among the values
-    // are added to the rows that see them (p > 0 times one is one) and leave the tile before the product.
-    const bool inside = ((now.half[0].page | now.half[1].page) >= 0) & (last <= wg_first) & ((first > wg_last - window) | (last < a.sinks));
-    if (!inside) {
+    if (!kLast && !inside(next)) hide(sc_next, next);
+    // 0 * NaN is NaN: in a tile that not every row of the workgroup sees all of, infinities and NaN among the values leave
+    // before the product; the rows that see them get them at the end
+    if (!inside(now)) {
       constexpr int kQuarter = kTileBytes / 4;
       char* vb = lds_v + kBuf * kTileBytes;
       uint32_t bad = 0;
@@ -965,25 +981,8 @@ __global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(
       tile_barrier();
       const int special = uniform(s_special[kBuf][0] | s_special[kBuf][1] | s_special[kBuf][2] | s_special[kBuf][3]);
       if (special != 0) {
-        if (!none) {
+        specials = true;
 #pragma unroll 1
-          for (int j = 0; j < kChunkKeys; ++j) {
-            const int key = first + j;
-            const bool s = ((j < 32 ? now.half[0].page : now.half[1].page) >= 0) & (key <= row_pos) & ((key > row_pos - window) | (key < a.sinks));
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-              for (int q = 0; q < 4; ++q) {               // dims dt * 32 + q * 8 + hf * 4 ..+3
-                const uint2 w = *reinterpret_cast<const uint2*>(vb + j * kRow + (((dt * 4 + q) ^ (v_row_swizzle<D>(j) << 2)) << 4) + hf * 8);
-                const float y[4] = {__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u), __uint_as_float(w.y << 16),
-                                    __uint_as_float(w.y & 0xFFFF0000u)};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[dt][4 * q + e] += s & !(fabsf(y[e]) < INFINITY) ? y[e] : 0.f;
-              }
-          }
-        }
-        tile_barrier();
-#pragma unroll
         for (int i = 0; i < kQuarter / 1024; ++i) {
           u32x4* w = reinterpret_cast<u32x4*>(vb + wave * kQuarter + i * 1024 + lane * 16);
           *w = u32x4{without_specials<false>((*w)[0]), without_specials<false>((*w)[1]), without_specials<false>((*w)[2]), without_specials<false>((*w)[3])};
@@ -992,10 +991,12 @@ __global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(
       }
     }
 
-    // ---- O^T += V^T P^T ----
-    if (!none) {
-      __builtin_amdgcn_s_setprio(1);
-      constexpr int kSteps = DT * KT * 2;
+    __builtin_amdgcn_s_setprio(1);
+    float mx[KT];
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) mx[kt] = -INFINITY;
+    {
+      constexpr int kSteps = DT * KT * 2, kScores = 16 * KT;
       static_assert(kSteps >= kDepth, "pipeline deeper than the phase");
       bf16x8 fr[kDepth];
 #pragma unroll
@@ -1006,37 +1007,110 @@ __global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(
         const int dt = i % DT, st = i / DT;
         o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[i % kDepth], pf[st >> 1][st & 1], o[dt], 0, 0, 0);
         if (i + kDepth < kSteps) fr[i % kDepth] = v_frag((i + kDepth) % DT, (i + kDepth) / DT, kBuf);
+        if (!kLast) {
+#pragma unroll
+          for (int e = i * kScores / kSteps; e < (i + 1) * kScores / kSteps; ++e) mx[e >> 4] = fmaxf(mx[e >> 4], sc_next[e >> 4][e & 15]);
+        }
         __builtin_amdgcn_sched_barrier(0);
       }
     }
     __builtin_amdgcn_s_setprio(0);
-    if (kE4m3 && more) deliver(1 - kBuf);
-    wait_async_loads();                                   // this wave's share of the next tile has landed
-    tile_barrier();                                       // ... everyone's, and everyone is done with this one
-    now = next;
+    if (!kLast) {
+      raise(mx, next);
+      if (kE4m3) {
+        deliver_v(1 - kBuf, next);
+        if (two) deliver_k(kBuf);
+      }
+      wait_async_loads();                                 // this wave's share of the tiles ahead has landed
+      tile_barrier();                                     // ... everyone's, and everyone is done with this tile
+      now = next;
+      next = after;
+    }
   };
 
   if (c0 < c1) {
+    // K and V of the first tile, K of the second
     now = locate(c0);
+    if (c0 + 1 < c1) next = locate(c0 + 1);
     if (kE4m3) {
-      request();
-      deliver(0);
+      request(kx, a.cache.k, now);
+      request(vx, a.cache.v, now);
+      deliver_k(0);
+      deliver_v(0, now);
+      if (c0 + 1 < c1) {
+        request(kx, a.cache.k, next);
+        deliver_k(1);
+      }
     } else {
+      TileRsrc krs[2], vrs[2];
+      resources(krs, a.cache.k, now);
+      resources(vrs, a.cache.v, now);
 #pragma unroll
-      for (int i = 0; i < kPieces; ++i) copy_k(i, 0);
+      for (int i = 0; i < kPieces; ++i) copy_k(krs, i, 0);
 #pragma unroll
-      for (int i = 0; i < kPieces; ++i) copy_v(i, 0);
+      for (int i = 0; i < kPieces; ++i) copy_v(vrs, i, 0);
+      if (c0 + 1 < c1) {
+        resources(krs, a.cache.k, next);
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) copy_k(krs, i, 1);
+      }
     }
     wait_async_loads();
     tile_barrier();
-    int i = c0;
-    for (; i + 1 < c1; i += 2) {
-      step(std::integral_constant<int, 0>{}, i);
-      step(std::integral_constant<int, 1>{}, i + 1);
+    scores(sa, std::integral_constant<int, 0>{}, [](int) {});
+    if (!inside(now)) hide(sa, now);
+    {
+      float mx[KT];
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt) {
+        mx[kt] = sa[kt][0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) mx[kt] = fmaxf(mx[kt], sa[kt][r]);
+      }
+      raise(mx, now);
     }
-    if (i < c1) step(std::integral_constant<int, 0>{}, i);
+    tile_barrier();                                       // everyone is done with K of the first tile
+    int i = c0;
+    for (; i + 2 < c1; i += 2) {
+      step(std::integral_constant<int, 0>{}, std::false_type{}, sa, sb, i);
+      step(std::integral_constant<int, 1>{}, std::false_type{}, sb, sa, i + 1);
+    }
+    if (i + 1 < c1) {
+      step(std::integral_constant<int, 0>{}, std::false_type{}, sa, sb, i);
+      step(std::integral_constant<int, 1>{}, std::true_type{}, sb, sa, i + 1);
+    } else {
+      step(std::integral_constant<int, 0>{}, std::true_type{}, sa, sb, i);
+    }
   }
 
+  if (specials) {                                         // rare: the tiles once more; p > 0 times an infinity or NaN is that
+#pragma unroll 1
+    for (int i = c0; i < c1; ++i) {
+      const Tile x = locate(i);
+      if (inside(x)) continue;
+#pragma unroll 1
+      for (int j = 0; j < kChunkKeys; ++j) {
+        constexpr int kElem = kE4m3 ? 1 : 2;
+        const Half& y = j < 32 ? x.half[0] : x.half[1];
+        const int key = x.first + j;
+        const bool s = (y.page >= 0) & (key <= row_pos) & ((key > row_pos - window) | (key < a.sinks));
+        if (!s) continue;
+        const char* vr = a.cache.v + y.off + (j & 31) * (D * kElem);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const char* at = vr + (dt * 32 + 8 * (r >> 2) + 4 * hf + (r & 3)) * kElem;
+            float z;
+            if constexpr (kE4m3)
+              z = __builtin_amdgcn_cvt_f32_fp8(*reinterpret_cast<const uint8_t*>(at), 0);
+            else
+              z = bf16_bits_to_float(*reinterpret_cast<const uint16_t*>(at));
+            o[dt][r] += fabsf(z) < INFINITY ? 0.f : z;
+          }
+      }
+    }
+  }
   const float l = other_half_sum(l_run);
   if (wave_row0 + l32 >= c.rows) return;
   if (splits == 1) {
