@@ -919,7 +919,7 @@ __global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(
     float by[KT];
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) by[kt] = kE4m3 ? a.scale * now.half[kt].ks : a.scale;
-    bf16x8 pf[KT][2];
+    u32x4 pf[KT][2];
     float sum0 = 0.f, sum1 = 0.f;
     auto phase1 = [&](auto scaled) __attribute__((always_inline)) {
       auto pair = [&](int e) __attribute__((always_inline)) {       // scores 2e, 2e + 1 of this lane
@@ -932,10 +932,9 @@ __global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(
           p0 *= now.half[kt].vs;
           p1 *= now.half[kt].vs;
         }
-        const f32x2 pp = {p0, p1};
-        const bf16x2 pb = __builtin_convertvector(pp, bf16x2);
-        pf[kt][r >> 3][r & 7] = pb[0];
-        pf[kt][r >> 3][(r & 7) + 1] = pb[1];
+        uint32_t w = bf16_pair(p0, p1);
+        asm volatile("" : "+v"(w), "+v"(sum0), "+v"(sum1));         // here, not where the compiler first needs it
+        pf[kt][r >> 3][(r & 7) >> 1] = w;
       };
       constexpr int kPairs = 8 * KT;
       if constexpr (kLast) {
@@ -1005,7 +1004,7 @@ __global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(
 #pragma unroll
       for (int i = 0; i < kSteps; ++i) {
         const int dt = i % DT, st = i / DT;
-        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[i % kDepth], pf[st >> 1][st & 1], o[dt], 0, 0, 0);
+        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[i % kDepth], __builtin_bit_cast(bf16x8, pf[st >> 1][st & 1]), o[dt], 0, 0, 0);
         if (i + kDepth < kSteps) fr[i % kDepth] = v_frag((i + kDepth) % DT, (i + kDepth) / DT, kBuf);
         if (!kLast) {
 #pragma unroll
