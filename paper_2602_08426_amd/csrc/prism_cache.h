@@ -7,6 +7,9 @@
 namespace prism {
 
 constexpr int kMaxPairs = kMaxHeadDim / 2;
+constexpr int kMaxTokens = 1 << 28;             // of a call: 32-bit row numbers and grids
+constexpr int kMaxSeqs = 1 << 24;
+constexpr int kMaxHeads = 1 << 14;              // Q, K and V heads together are a grid's second dimension
 constexpr float kE4m3Max = 448.f;
 constexpr int kMinScaleExponent = -120;         // of a page and head that holds zeros only
 
@@ -86,6 +89,7 @@ inline int check_cache(const prism_cache* c) {
   if (!known_head_dim(c->head_dim) || (c->page != 32 && c->page != 64 && c->page != 128)) return PRISM_ERR_UNSUPPORTED;
   if (c->dtype != PRISM_CACHE_BF16 && c->dtype != PRISM_CACHE_E4M3) return PRISM_ERR_UNSUPPORTED;
   if (c->n_pages <= 0 || c->n_kv_heads <= 0) return PRISM_ERR_INVALID_ARG;
+  if (c->n_kv_heads > kMaxHeads) return PRISM_ERR_UNSUPPORTED;
   const int64_t least = (int64_t)c->n_kv_heads * c->page * c->head_dim;
   if (c->page_stride != 0 && (c->page_stride < least || c->page_stride % 16 != 0 || c->page_stride > ((int64_t)1 << 60) / c->n_pages))
     return PRISM_ERR_INVALID_ARG;
@@ -101,7 +105,7 @@ inline int check_batch(const prism_cache* c, const prism_batch* b) {
   if (b == nullptr) return PRISM_ERR_INVALID_ARG;
   if (b->n_seqs < 0 || b->n_tokens < 0 || b->max_tokens <= 0 || b->max_pages <= 0) return PRISM_ERR_INVALID_ARG;
   if ((int64_t)b->max_pages * c->page > 1 << 30) return PRISM_ERR_UNSUPPORTED;        // positions and their sums stay in 32 bits
-  if (b->n_tokens > 1 << 28 || b->n_seqs > 1 << 24) return PRISM_ERR_UNSUPPORTED;
+  if (b->n_tokens > kMaxTokens || b->n_seqs > kMaxSeqs) return PRISM_ERR_UNSUPPORTED;
   if (b->n_tokens == 0) return PRISM_OK;
   if (b->n_seqs == 0 || b->lengths == nullptr || b->page_table == nullptr) return PRISM_ERR_INVALID_ARG;
   if (b->cu_tokens == nullptr && (int64_t)b->n_seqs * b->max_tokens != b->n_tokens) return PRISM_ERR_INVALID_ARG;

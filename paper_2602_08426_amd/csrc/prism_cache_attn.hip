@@ -729,15 +729,20 @@ __global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(
     v_lane[i] = r * kRow + (((t % kCpr) ^ (v_row_swizzle<D>(r) << 2)) << 4);
   }
 
-  // ---- tiles: entries of the page table (and scales) held 64 a time, one a lane ----
+  // ---- tiles: entries of the page table held 64 a time, one a lane, as addresses of the head's K (0: no page), with scales ----
   const int32_t* table = a.batch.table + (int64_t)c.s * a.batch.max_pages;
-  int held_from = -64, held = 0;
+  constexpr int kPageRow = kE4m3 ? D : kRow;
+  const char* k_head = a.cache.k + (int64_t)kv * a.cache.page * kPageRow;
+  const int64_t v_from_k = a.cache.v - a.cache.k;
+  int held_from = -64;
+  uint32_t held_lo = 0, held_hi = 0;
   float held_ks = 0.f, held_vs = 0.f;
+  auto lane_value = [](uint32_t x, int lane) __attribute__((always_inline)) { return (uint32_t)__builtin_amdgcn_readlane((int)x, lane); };
   // e4m3: the values' scale is a power of two, which the conversion to bf16 applies, times vs in [1, 2): 1 for scales of
   // prism_cache_append, and the probabilities need no factor.
   struct Half {
-    int page, bytes;                                      // page < 0: none; bytes that are there: what lies behind reads as zero
-    int64_t off;                                          // in K and in V
+    uint64_t k;                                           // address of its K; V lies v_from_k behind
+    int bytes;                                            // that are there: what lies behind reads as zero; 0: no page
     float ks, vs, v_power;
   };
   struct Tile {
@@ -753,33 +758,37 @@ __global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(
       if ((unsigned)(e - held_from) >= 64u) {
         held_from = e;
         const int mine = e + lane;
-        held = mine < a.batch.max_pages ? table[mine] : -1;
-        if (held >= a.cache.n_pages) held = -1;
+        const int id = mine < a.batch.max_pages ? table[mine] : -1;
+        const bool there = id >= 0 && id < a.cache.n_pages;
+        const uint64_t at = there ? (uint64_t)k_head + (uint64_t)id * a.cache.page_stride : 0;
+        held_lo = (uint32_t)at;
+        held_hi = (uint32_t)(at >> 32);
         if (kE4m3) {
-          const int64_t sc = (int64_t)max(held, 0) * h_kv + kv;
+          const int64_t sc = (int64_t)(there ? id : 0) * h_kv + kv;
           held_ks = a.cache.k_scale[sc];
           held_vs = a.cache.v_scale[sc];
         }
       }
       Half& y = x.half[hv];
-      y.page = __builtin_amdgcn_readlane(held, e - held_from);
+      const int l = e - held_from;
+      const uint64_t at = (uint64_t)lane_value(held_hi, l) << 32 | lane_value(held_lo, l);
+      y.k = at + (tk & (a.cache.page - 1)) * kPageRow;
+      const int there = c.r.length - tk;
+      y.bytes = at == 0 || there <= 0 ? 0 : (there >= 32 ? 32 : there) * kPageRow;
       if (kE4m3) {
-        y.ks = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, held_ks), e - held_from));
-        const int vs = __builtin_amdgcn_readlane(__builtin_bit_cast(int, held_vs), e - held_from);
-        y.vs = __builtin_bit_cast(float, (vs & 0x007FFFFF) | 0x3F800000);
-        y.v_power = __builtin_bit_cast(float, vs & 0x7F800000);
+        y.ks = __uint_as_float(lane_value(__float_as_uint(held_ks), l));
+        const uint32_t vs = lane_value(__float_as_uint(held_vs), l);
+        y.vs = __uint_as_float((vs & 0x007FFFFFu) | 0x3F800000u);
+        y.v_power = __uint_as_float(vs & 0x7F800000u);
       }
-      constexpr int kPageRow = kE4m3 ? D : kRow;
-      y.off = max(y.page, 0) * a.cache.page_stride + (int64_t)(kv * a.cache.page + (tk & (a.cache.page - 1))) * kPageRow;
-      y.bytes = y.page < 0 ? 0 : max(min(32, c.r.length - tk), 0) * kPageRow;
     }
     return x;
   };
   const int wave_base = uniform(t & ~63);
   // piece i of K or V of a tile (its halves' resources), to buffer b
-  auto resources = [&](TileRsrc(&rs)[2], const char* base, const Tile& x) __attribute__((always_inline)) {
+  auto resources = [&](TileRsrc(&rs)[2], const Tile& x, int64_t from_k) __attribute__((always_inline)) {
 #pragma unroll
-    for (int hv = 0; hv < 2; ++hv) rs[hv] = make_tile_rsrc(base + x.half[hv].off, x.half[hv].bytes);
+    for (int hv = 0; hv < 2; ++hv) rs[hv] = make_tile_rsrc((const void*)(x.half[hv].k + from_k), x.half[hv].bytes);
   };
   auto copy_k = [&](const TileRsrc(&rs)[2], int i, int b) __attribute__((always_inline)) {
     const int j = i % kHalf;
@@ -793,11 +802,11 @@ __global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(
   u32x4 kx[kWide > 0 ? kWide : 1], vx[kWide > 0 ? kWide : 1];
   constexpr int kWideCpr = D / 16, kWideRp = kChunkThreads / kWideCpr;    // rows of a piece of all threads: 64, 32, 16
   auto wide_half = [&](int i) __attribute__((always_inline)) { return kWideRp == 64 ? uniform(t / kWideCpr >> 5) : i * kWideRp / 32; };
-  auto request = [&](u32x4(&to)[kWide > 0 ? kWide : 1], const char* base, const Tile& x) __attribute__((always_inline)) {
+  auto request = [&](u32x4(&to)[kWide > 0 ? kWide : 1], const Tile& x, int64_t from_k) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < kWide; ++i) {
       const int r = i * kWideRp + t / kWideCpr, hv = wide_half(i);
-      to[i] = __builtin_amdgcn_raw_buffer_load_b128(make_rsrc(base + (hv ? x.half[1].off : x.half[0].off), hv ? x.half[1].bytes : x.half[0].bytes),
+      to[i] = __builtin_amdgcn_raw_buffer_load_b128(make_rsrc((const void*)((hv ? x.half[1].k : x.half[0].k) + from_k), hv ? x.half[1].bytes : x.half[0].bytes),
                                                     (r & 31) * D + (t % kWideCpr) * 16, 0, 0);
     }
   };
@@ -858,7 +867,7 @@ __global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(
   };
   // whether all rows of the workgroup see all of a tile
   auto inside = [&](const Tile& x) __attribute__((always_inline)) {
-    return ((x.half[0].page | x.half[1].page) >= 0) & (x.first + kChunkKeys - 1 <= wg_first) &
+    return (x.half[0].bytes != 0) & (x.half[1].bytes != 0) & (x.first + kChunkKeys - 1 <= wg_first) &
            ((x.first > wg_last - window) | (x.first + kChunkKeys - 1 < a.sinks));
   };
   // scores of keys that a row does not see (without branches, as in step_kernel)
@@ -870,7 +879,7 @@ __global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int key = x.first + kt * 32 + 8 * (r >> 2) + 4 * hf + (r & 3);
-        const bool s = (x.half[kt].page >= 0) & (key <= pos) & ((key > pos - window) | (key < a.sinks));
+        const bool s = (x.half[kt].bytes != 0) & (key <= pos) & ((key > pos - window) | (key < a.sinks));
         sc[kt][r] = s ? sc[kt][r] : -INFINITY;
       }
   };
@@ -908,11 +917,11 @@ __global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(
     if (!kLast) {
       if (two) after = locate(list_at + 2);
       if (kE4m3) {
-        request(vx, a.cache.v, next);
-        if (two) request(kx, a.cache.k, after);
+        request(vx, next, v_from_k);
+        if (two) request(kx, after, 0);
       } else {
-        resources(vrs, a.cache.v, next);
-        resources(krs, a.cache.k, after);
+        resources(vrs, next, v_from_k);
+        resources(krs, after, 0);
       }
     }
     const float base = m_run == -INFINITY ? 0.f : m_run;  // nothing seen yet: all p are 0
@@ -1032,24 +1041,24 @@ __global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(
     now = locate(c0);
     if (c0 + 1 < c1) next = locate(c0 + 1);
     if (kE4m3) {
-      request(kx, a.cache.k, now);
-      request(vx, a.cache.v, now);
+      request(kx, now, 0);
+      request(vx, now, v_from_k);
       deliver_k(0);
       deliver_v(0, now);
       if (c0 + 1 < c1) {
-        request(kx, a.cache.k, next);
+        request(kx, next, 0);
         deliver_k(1);
       }
     } else {
       TileRsrc krs[2], vrs[2];
-      resources(krs, a.cache.k, now);
-      resources(vrs, a.cache.v, now);
+      resources(krs, now, 0);
+      resources(vrs, now, v_from_k);
 #pragma unroll
       for (int i = 0; i < kPieces; ++i) copy_k(krs, i, 0);
 #pragma unroll
       for (int i = 0; i < kPieces; ++i) copy_v(vrs, i, 0);
       if (c0 + 1 < c1) {
-        resources(krs, a.cache.k, next);
+        resources(krs, next, 0);
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) copy_k(krs, i, 1);
       }
@@ -1092,9 +1101,9 @@ __global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(
         constexpr int kElem = kE4m3 ? 1 : 2;
         const Half& y = j < 32 ? x.half[0] : x.half[1];
         const int key = x.first + j;
-        const bool s = (y.page >= 0) & (key <= row_pos) & ((key > row_pos - window) | (key < a.sinks));
+        const bool s = (y.bytes != 0) & (key <= row_pos) & ((key > row_pos - window) | (key < a.sinks));
         if (!s) continue;
-        const char* vr = a.cache.v + y.off + (j & 31) * (D * kElem);
+        const char* vr = (const char*)(y.k + v_from_k) + (j & 31) * (D * kElem);
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -1219,7 +1228,9 @@ static int check_attn(const prism_cache* cache, const prism_batch* batch, int n_
   int rc = check_cache(cache);
   if (rc != PRISM_OK || (rc = check_batch(cache, batch)) != PRISM_OK) return rc;
   if (n_q_heads <= 0 || n_q_heads % cache->n_kv_heads != 0) return PRISM_ERR_INVALID_ARG;
-  if (n_q_heads > 1 << 16 || cache->n_kv_heads > 1 << 15) return PRISM_ERR_UNSUPPORTED;
+  if (n_q_heads > kMaxHeads) return PRISM_ERR_UNSUPPORTED;
+  // rows and (sequence, kv head) pairs are counted in 32 bits
+  if ((int64_t)batch->n_tokens * n_q_heads > 1 << 30 || (int64_t)batch->n_seqs * cache->n_kv_heads > 1 << 24) return PRISM_ERR_UNSUPPORTED;
   return PRISM_OK;
 }
 
