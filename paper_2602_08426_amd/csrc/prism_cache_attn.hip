@@ -883,13 +883,16 @@ __global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(
         sc[kt][r] = s ? sc[kt][r] : -INFINITY;
       }
   };
-  // the running maximum (mx: this lane's of each 32 keys), and everything that was scaled by the one before
+  // The reference of the exponentials (mx: this lane's maximum of each 32 keys).  It follows the maximum only when that is more than
+  // 2^8 ahead, so that the sums are seldom rescaled: p stays below 2^8, whose rounding to bf16 is as good, and the sums
+  // are far from the end of fp32.
   auto raise = [&](const float (&mx)[KT], const Tile& x) __attribute__((always_inline)) {
     float y = -INFINITY;
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) y = fmaxf(y, mx[kt] * (kE4m3 ? a.scale * x.half[kt].ks : a.scale));
-    const float m_new = fmaxf(m_run, other_half_max(y));
-    if (__builtin_amdgcn_ballot_w64(m_new > m_run) != 0) {          // some row's maximum moved
+    y = other_half_max(y);
+    if (__builtin_amdgcn_ballot_w64(y > m_run + 8.f) != 0) {        // some row is that far ahead
+      const float m_new = fmaxf(m_run, y);
       const float keep = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
       l_run *= keep;
 #pragma unroll
