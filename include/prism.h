@@ -422,7 +422,7 @@ typedef struct prism_batch {
   const int32_t* page_table;   /* device, [n_seqs, max_pages] */
 } prism_batch;
 
-/* Stores K and V [n_kv_heads, n_tokens, d] of the new tokens.  `rotary` (may be NULL: K is stored as it is) rotates
+/* Stores K and V [n_kv_heads, n_tokens, d] of the new tokens.  `rotary` (may be NULL: everything as it is) rotates
  * K by the tokens' positions on the way, and with q_in and q_out not NULL also Q [n_q_heads, n_tokens, d] (q_out may be
  * q_in).  Values are rounded once, from fp32.
  * PRISM_CACHE_E4M3: the scale of a page and head is the smallest power of two (at least 2^-120) with which all finite

@@ -356,7 +356,7 @@ extern "C" int prism_cache_append(const prism_cache* cache, const prism_batch* b
   const int d = cache->head_dim, T = batch->n_tokens, h_kv = cache->n_kv_heads;
   if (rotary != nullptr && (rc = check_rotary(rotary, d)) != PRISM_OK) return rc;
   const bool with_q = q_in != nullptr || q_out != nullptr;
-  if (n_q_heads < 0 || (with_q && (rotary == nullptr || n_q_heads == 0))) return PRISM_ERR_INVALID_ARG;
+  if (n_q_heads < 0 || (with_q && n_q_heads == 0)) return PRISM_ERR_INVALID_ARG;
   if (n_q_heads > kMaxHeads) return PRISM_ERR_UNSUPPORTED;
   if (T == 0) return PRISM_OK;
   if ((rc = check_cache_memory(cache)) != PRISM_OK || (rc = check_rows(k, h_kv, T, d, false)) != PRISM_OK ||

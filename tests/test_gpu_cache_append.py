@@ -53,17 +53,19 @@ def test_bf16(h, h_kv, d, page, rot, half, lengths, news, behind, how):
     cache = pb.make_cache(kp, vp)
     batch = pb.make_batch(su.ints(lengths), su.ints(table), max(news), su.ints(cu), rows)
     qd, kd, vd = (su.layout_of(su.to_device(x), how) for x in (q, k, v))
-    qo = torch.full((h, rows, d), 9.0, dtype=torch.bfloat16, device="cuda") if rot else None
-    pb.prism_cache_append(cache, batch, _rotary(rot, half) if rot else None, kd, vd, qd if rot else None, qo)
+    qo = torch.full((h, rows, d), 9.0, dtype=torch.bfloat16, device="cuda")
+    pb.prism_cache_append(cache, batch, _rotary(rot, half) if rot else None, kd, vd, qd, qo)
     torch.cuda.synchronize()
     pos, turned, slack = _positions(lengths, cu, rows), k, np.zeros_like(k)
+    mine = np.arange(rows) < cu[-1]
     if rot:
         theta = so.frequencies(BASE, rot)
         turned, slack = so.rotate(k, pos, theta, half), su.TURN * so.pair_magnitude(k, rot, half)
-        mine = np.arange(rows) < cu[-1]
         su.check_bf16(su.host(qo)[:, mine], so.rotate(q, pos, theta, half)[:, mine],
                       su.TURN * so.pair_magnitude(q, rot, half)[:, mine], "q")
-        assert (su.host(qo)[:, ~mine] == 9.0).all()                       # rows behind the last sequence
+    else:
+        assert np.array_equal(su.host(qo)[:, mine], q[:, mine])
+    assert (su.host(qo)[:, ~mine] == 9.0).all()                           # rows behind the last sequence
     su.check_bf16(su.host(kp), so.append_bf16(old[0], turned, lengths, cu, table),
                   so.append_bf16(np.zeros_like(old[0]), slack, lengths, cu, table), "k")
     assert np.array_equal(su.host(vp), so.append_bf16(old[1], v, lengths, cu, table))

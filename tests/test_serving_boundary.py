@@ -125,8 +125,8 @@ def test_append_refusals(lib):
         assert append(lib, r=rotary(), h=4, q=rows(data=FAKE * 2), qo=rows(**kw)) == -1, kw
     for kw in BAD_OUT:
         assert append(lib, r=rotary(), h=4, q=rows(), qo=rows(data=FAKE * 2, **kw)) == -1, kw
-    assert append(lib, h=4, q=rows(), qo=rows()) == -1                        # Q without a rotation
-    assert append(lib, r=rotary(), h=4, q=rows()) == -1                       # ... without its output
+    assert append(lib, r=rotary(), h=4, q=rows()) == -1                       # Q without its output
+    assert append(lib, h=4, qo=rows()) == -1
     assert append(lib, r=rotary(), h=0, q=rows(), qo=rows()) == -1
     assert append(lib, h=-1) == -1 and append(lib, h=(1 << 16) + 1) == -2
     assert append(lib, c=cache(n_kv_heads=(1 << 15) + 1)) == -2
