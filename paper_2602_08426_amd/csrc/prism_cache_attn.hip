@@ -616,64 +616,188 @@ __global__ __launch_bounds__(kStepThreads) void combine_kernel(AttnCall a, StepW
 // on the way from LDS.  bf16 pages are copied to LDS asynchronously; e4m3 pages pass through registers, where they
 // become bf16 once for the four waves (their scales go to the scores and the probabilities in fp32).
 // Rows of a kv head's q-heads lie side by side, so the 128 rows are 128 / g tokens and the diagonal costs little.
-// Where the row tiles are few, each is cut into `splits` parts of its keys, and chunk_combine_kernel joins them.
+// Where the row tiles are few, they are cut into pieces, which chunk_combine_kernel joins: each into the same number of them, or,
+// where sequences of different lengths may be long, by chunk_plan_kernel, one workgroup, which counts the keys and deals.
 // =====================================================================================
 constexpr int kChunkRows = 128, kChunkKeys = 64, kChunkThreads = 256;
 
+// How the row tiles (slots) are cut.  splits > 0: into so many pieces each.  Otherwise what chunk_plan_kernel leaves: of a slot its
+// sequence, its first piece, counted over a kv head, and where its parts lie if it has several; the slots that have several.
+struct ChunkPlan {
+  int32_t* first_piece;    // [slots + 1]
+  int32_t* seq;            // [slots]
+  int32_t* first_part;     // [slots]
+  int32_t* cut;            // [slots]
+  int32_t* head;           // tiles of a piece at most, parts of a kv head, slots that are cut
+  int32_t slots, splits;
+};
+// Of a piece its slot, its sequence, which of the slot's pieces it is, and its place among the kv head's parts.
+struct ChunkPiece {
+  int slot, seq, nth, part;
+};
 struct ChunkWs {
-  float* part;             // [workgroups][128][D] unscaled sums
-  float2* stats;           // [workgroups][128]
+  float* part;             // [kv heads][parts][part_rows][D] unscaled sums
+  float2* stats;           // [kv heads][parts][part_rows]
+  ChunkPlan plan;
+  int32_t part_rows;       // rows of a row tile at most
 };
-// Where a workgroup's rows are: kv head, row tile of all sequences, part.  Workgroups go round the eight XCDs; those of an XCD
-// get the same kv heads, whose keys then stay in its L2.  Later row tiles, which see more keys, first.
-struct ChunkPlace {
-  int kv, slot, split;
-};
-__device__ __forceinline__ ChunkPlace chunk_place(int b, int h_kv, int slots, int splits) {
-  ChunkPlace p;
+// Workgroups go round the eight XCDs; those of an XCD get the same kv heads, whose keys then stay in its L2.  Later row tiles,
+// which see more keys, first.  Returns the piece of kv head *kv, or -1.
+__device__ __forceinline__ int chunk_piece(int b, int h_kv, int pieces, int* kv) {
+  int j;
   if (8 % h_kv == 0) {                                    // 8 / h_kv XCDs share a kv head
     const int share = 8 / h_kv, x = b & 7;
-    p.kv = x / share;
-    const int i = (b >> 3) * share + x % share;
-    p.slot = i / splits;
-    p.split = i % splits;
+    *kv = x / share;
+    j = (b >> 3) * share + x % share;
   } else if (h_kv % 8 == 0) {
-    const int i = b >> 3, per = slots * splits;
-    p.kv = (b & 7) + 8 * (i / per);
-    p.slot = i % per / splits;
-    p.split = i % splits;
+    const int i = b >> 3;
+    if (pieces == 0 || i / pieces >= h_kv / 8) return -1;
+    *kv = (b & 7) + 8 * (i / pieces);
+    j = i % pieces;
   } else {
-    p.kv = b % h_kv;
-    p.slot = b / h_kv / splits;
-    p.split = b / h_kv % splits;
+    *kv = b % h_kv;
+    j = b / h_kv;
   }
-  p.slot = slots - 1 - p.slot;
-  return p;
+  return pieces - 1 - j;                                  // below 0: none
 }
-__host__ __device__ inline int chunk_grid(int h_kv, int slots, int splits) {
+inline int64_t chunk_grid(int h_kv, int64_t pieces) {
   const int share = 8 % h_kv == 0 ? 8 / h_kv : 1;
-  return (slots * splits + share - 1) / share * share * h_kv;
+  return (pieces + share - 1) / share * share * h_kv;
 }
 // The rows of a slot; rows == 0: none, or not this kernel's.
 struct ChunkRows {
   SeqRows r;
   int s, row0, rows;       // first row, rows of the sequence
 };
-__device__ __forceinline__ ChunkRows chunk_rows(const AttnCall& a, int slot) {
+__device__ __forceinline__ ChunkRows chunk_rows(const AttnCall& a, int slot, int s) {
   ChunkRows c;
-  c.s = uniform(seq_at(a.batch, slot, a.g, 7, 1));
+  c.s = s;
   c.r = seq_rows(a.batch, c.s);
-  c.r.row0 = uniform(c.r.row0);
-  c.r.n = uniform(c.r.n);
-  c.r.length = uniform(c.r.length);
   c.row0 = (slot - (int)((((int64_t)c.r.row0 * a.g) >> 7) + c.s)) * kChunkRows;
   const int rows = min(c.r.n, a.batch.each) * a.g;
   c.rows = rows > a.step_rows && c.row0 >= 0 && c.row0 < rows ? rows : 0;
   return c;
 }
 
+__device__ __forceinline__ ChunkRows chunk_rows(const AttnCall& a, int slot) { return chunk_rows(a, slot, seq_at(a.batch, slot, a.g, 7, 1)); }
+__device__ __forceinline__ ChunkRows uniform(ChunkRows c) {
+  return ChunkRows{{uniform(c.r.row0), uniform(c.r.n), uniform(c.r.length)}, uniform(c.s), uniform(c.row0), uniform(c.rows)};
+}
+__device__ __forceinline__ KeyRange chunk_keys(const AttnCall& a, const ChunkRows& c) {
+  if (c.rows == 0) return KeyRange{0, 0, 0};
+  const int pos0 = c.r.length - c.r.n, last = min(c.row0 + kChunkRows, c.rows) - 1;
+  return key_range<kChunkKeys>(a, pos0 + c.row0 / a.g, pos0 + last / a.g);
+}
+__device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
+
+// A piece is at most 5/4 of the share that each of `workers` workgroups would have of all tiles, and four tiles at least.  A row tile
+// is cut into equal pieces, each more than half of that, so that the pieces of cut row tiles are fewer than 8/5 of the workers.
+// Measured (one of 1024 tokens at 32K beside prompts of 2000, 1000 and 500, 32/8 heads, d = 128; 6 ragged ones up to 32K, 16/4 heads,
+// d = 64): 2 shares 827 and 177 us, 3/2 569 and 200, 5/4 570 and 183; cut evenly 813 and 508.
+constexpr int kPlanThreads = 1024, kLeastPiece = 4;
+template <int D>
+__global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(AttnCall a, ChunkPlan plan, int workers) {
+  __shared__ int s_sum[3][kPlanThreads / 64];
+  __shared__ unsigned long long s_total;
+  __shared__ int s_blind[kPlanThreads], s_blinds;
+  const int t = threadIdx.x, wave = t >> 6;
+  if (t == 0) s_total = 0;
+  __syncthreads();
+  ChunkRows c = {};                                       // of the last slot that was counted
+  int tiles = 0;
+  unsigned long long mine = 0;
+  for (int slot = t; slot < plan.slots; slot += kPlanThreads) {
+    c = chunk_rows(a, slot);
+    tiles = chunk_keys(a, c).count();
+    mine += (unsigned)tiles;
+  }
+  atomicAdd(&s_total, mine);                              // whole numbers: in any order
+  __syncthreads();
+  const unsigned long long all = s_total * a.cache.h_kv;
+  const int most = max(kLeastPiece, (int)((5 * all + 4 * workers - 1) / (4 * workers)));
+  int carry[3] = {0, 0, 0};                               // pieces, parts, cut slots in front
+  for (int base = 0; base < plan.slots; base += kPlanThreads) {
+    const int slot = base + t;
+    if (plan.slots > kPlanThreads) {
+      c = ChunkRows{};
+      if (slot < plan.slots) c = chunk_rows(a, slot);
+      tiles = chunk_keys(a, c).count();
+    }
+    const int pieces = ceil_div(tiles, most), cut = pieces > 1 ? 1 : 0;
+    const int own[3] = {pieces, cut * pieces, cut};
+    int upto[3];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) upto[i] = wave_scan_inclusive(own[i]);
+    __syncthreads();
+    if (t == 0) s_blinds = 0;
+    if ((t & 63) == 63)
+#pragma unroll
+      for (int i = 0; i < 3; ++i) s_sum[i][wave] = upto[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      int total = 0;
+      for (int w = 0; w < kPlanThreads / 64; ++w) {
+        if (w == wave) upto[i] += total;
+        total += s_sum[i][w];
+      }
+      upto[i] += carry[i];
+      carry[i] += total;
+    }
+    if (slot < plan.slots) {
+      plan.first_piece[slot] = upto[0] - own[0];
+      plan.seq[slot] = c.s;
+      plan.first_part[slot] = upto[1] - own[1];
+      if (cut) plan.cut[upto[2] - 1] = slot;
+    }
+    // rows that see nothing
+    if (c.rows > 0 && tiles == 0) s_blind[atomicAdd(&s_blinds, 1)] = slot;
+    __syncthreads();
+    for (int i = 0; i < s_blinds; ++i) {
+      const ChunkRows b = chunk_rows(a, s_blind[i]);
+      const int n = min(b.row0 + kChunkRows, b.rows) - b.row0;
+      for (int x = t; x < n * a.cache.h_kv * (D / 8); x += kPlanThreads) {
+        const int d0 = x % (D / 8) * 8, row = b.row0 + x / (D / 8) % n, kv = x / (D / 8) / n;
+        const int tok = row / a.g, hq = kv * a.g + row - tok * a.g;
+        *reinterpret_cast<uint4*>(a.out.p + (int64_t)hq * a.out.head + (int64_t)(b.r.row0 + tok) * a.out.token + d0) = make_uint4(0u, 0u, 0u, 0u);
+        if (a.lse != nullptr && d0 == 0) a.lse[(int64_t)hq * a.batch.n_tokens + b.r.row0 + tok] = -INFINITY;
+      }
+    }
+  }
+  if (t == 0) {
+    plan.first_piece[plan.slots] = carry[0];
+    plan.head[0] = most;
+    plan.head[1] = carry[1];
+    plan.head[2] = carry[2];
+  }
+}
+__device__ __forceinline__ int chunk_pieces(const ChunkPlan& plan) { return plan.splits > 0 ? plan.slots * plan.splits : plan.first_piece[plan.slots]; }
+__device__ __forceinline__ int chunk_parts(const ChunkPlan& plan) { return plan.splits > 0 ? plan.slots * plan.splits : plan.head[1]; }
+// Pieces of a slot with so many tiles of keys.
+__device__ __forceinline__ int chunk_pieces(const ChunkPlan& plan, int tiles) { return plan.splits > 0 ? plan.splits : ceil_div(tiles, plan.head[0]); }
+// A planned call's slot of piece j is the last one whose first piece is at most j.  64 places at a time.
+__device__ __forceinline__ ChunkPiece piece_at(const AttnCall& a, const ChunkPlan& plan, int j) {
+  if (plan.splits > 0) {
+    const int slot = j / plan.splits;
+    return ChunkPiece{slot, seq_at(a.batch, slot, a.g, 7, 1), j - slot * plan.splits, j};
+  }
+  const int lane = threadIdx.x & 63;
+  int lo = 0, n = plan.slots;                             // in [lo, lo + n), and lo's first piece is at most j
+  while (n > 1) {
+    const int step = ceil_div(n, 64), at = lo + lane * step;
+    const bool low = at < lo + n && plan.first_piece[at] <= j;
+    const int last = 63 - __builtin_clzll(__builtin_amdgcn_ballot_w64(low) | 1ull);
+    const int end = lo + n;
+    lo += last * step;
+    n = min(step, end - lo);
+  }
+  lo = uniform(lo);
+  const int nth = j - plan.first_piece[lo];
+  return ChunkPiece{lo, plan.seq[lo], nth, plan.first_part[lo] + nth};
+}
+
 template <int D, bool kE4m3>
-__global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(AttnCall a, ChunkWs ws, int slots, int splits) {
+__global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(AttnCall a, ChunkWs ws) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int KS = D / 16, DT = D / 32, KT = kChunkKeys / 32;
   constexpr int kRow = D * 2, kTileBytes = kChunkKeys * kRow, kSlab = 32 * kRow;
@@ -684,16 +808,19 @@ __global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(
   __shared__ __attribute__((aligned(16))) char lds_v[2 * kTileBytes];
   __shared__ int s_special[2][4];
   const int h_kv = a.cache.h_kv;
-  const ChunkPlace at = chunk_place(blockIdx.x, h_kv, slots, splits);
-  if (at.slot < 0) return;
-  const ChunkRows c = chunk_rows(a, at.slot);
+  const ChunkPlan& plan = ws.plan;
+  int kv = 0;
+  const int piece = chunk_piece(blockIdx.x, h_kv, chunk_pieces(plan), &kv);
+  if (piece < 0) return;
+  const ChunkPiece at = piece_at(a, plan, piece);
+  const ChunkRows c = uniform(chunk_rows(a, at.slot, at.seq));
   if (c.rows == 0) return;
   const int t = threadIdx.x, lane = t & 63, wave = uniform(t >> 6), l32 = lane & 31, hf = lane >> 5;
-  const int kv = at.kv, pos0 = c.r.length - c.r.n;
-  const int last_row = min(c.row0 + kChunkRows, c.rows) - 1;
+  const int pos0 = c.r.length - c.r.n, last_row = min(c.row0 + kChunkRows, c.rows) - 1;
   const int wg_first = pos0 + c.row0 / a.g, wg_last = pos0 + last_row / a.g;
-  const KeyRange keys = key_range<kChunkKeys>(a, wg_first, wg_last);
-  const int c0 = (int)((int64_t)keys.count() * at.split / splits), c1 = (int)((int64_t)keys.count() * (at.split + 1) / splits);
+  const KeyRange keys = chunk_keys(a, c);
+  const int pieces = chunk_pieces(plan, keys.count());
+  const int c0 = (int)((int64_t)keys.count() * at.nth / pieces), c1 = (int)((int64_t)keys.count() * (at.nth + 1) / pieces);
 
   // this wave's rows
   const int wave_row0 = c.row0 + wave * 32, row = min(wave_row0 + l32, c.rows - 1);
@@ -1124,7 +1251,7 @@ __global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(
   }
   const float l = other_half_sum(l_run);
   if (wave_row0 + l32 >= c.rows) return;
-  if (splits == 1) {
+  if (pieces == 1) {
     const float inv = l == 0.f ? 0.f : 1.f / l;
     uint16_t* op = a.out.p + (int64_t)hq * a.out.head + (int64_t)(c.r.row0 + tok) * a.out.token;
 #pragma unroll
@@ -1136,7 +1263,7 @@ __global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(
     if (a.lse != nullptr && hf == 0)
       a.lse[(int64_t)hq * a.batch.n_tokens + c.r.row0 + tok] = l == 0.f ? -INFINITY : (m_run + log2f(l)) * kLn2;
   } else {
-    const int64_t place = (((int64_t)kv * slots + at.slot) * splits + at.split) * kChunkRows + wave * 32 + l32;
+    const int64_t place = ((int64_t)kv * chunk_parts(plan) + at.part) * ws.part_rows + wave * 32 + l32;
     float* pp = ws.part + place * D;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
@@ -1148,26 +1275,82 @@ __global__ __launch_bounds__(kChunkThreads, D == 256 ? 1 : 2) void chunk_kernel(
 #endif
 }
 
-// Joins the parts of the rows: one workgroup for kChunkThreads * 4 / D rows.
-template <int D>
-__global__ __launch_bounds__(kChunkThreads) void chunk_combine_kernel(AttnCall a, ChunkWs ws, int slots, int splits) {
-  constexpr int kRows = kChunkThreads * 4 / D;
-  const int slot = blockIdx.x, kv = blockIdx.y;
-  const ChunkRows c = chunk_rows(a, slot);
-  const int x = blockIdx.z * kRows + threadIdx.x / (D / 4), d0 = threadIdx.x % (D / 4) * 4, row = c.row0 + x;
-  if (row >= c.rows) return;
-  const int64_t place = ((int64_t)kv * slots + slot) * splits * kChunkRows + x;
-  float top = -INFINITY;
-  for (int i = 0; i < splits; ++i) top = fmaxf(top, ws.stats[place + (int64_t)i * kChunkRows].x);
-  const float base = top == -INFINITY ? 0.f : top;
-  float sum = 0.f;
+// Joins the parts of the rows of cut row tiles.  The groups of D / 4 threads of a workgroup have a row each, or (kOneRow, for calls of
+// few row tiles, which have many parts) every so many parts of one row, each with a maximum of its own.
+template <int D, bool kOneRow>
+__global__ __launch_bounds__(kChunkThreads) void chunk_combine_kernel(AttnCall a, ChunkWs ws) {
+  constexpr int kGroups = kChunkThreads * 4 / D, kAtOnce = 4;
+  __shared__ float s_acc[kGroups][D];
+  __shared__ float s_top[kGroups], s_sum[kGroups];
+  const ChunkPlan& plan = ws.plan;
+  int slot = blockIdx.x, seq = 0, part = slot * plan.splits;
+  const int kv = blockIdx.y;
+  if (plan.splits > 0) {
+    seq = seq_at(a.batch, slot, a.g, 7, 1);
+  } else {
+    if (slot >= plan.head[2]) return;
+    slot = plan.cut[slot];
+    seq = plan.seq[slot];
+    part = plan.first_part[slot];
+  }
+  const ChunkRows c = uniform(chunk_rows(a, slot, seq));
+  if (c.rows == 0) return;
+  const int group = threadIdx.x / (D / 4), d0 = threadIdx.x % (D / 4) * 4;
+  const int x = kOneRow ? blockIdx.z : blockIdx.z * kGroups + group, row = c.row0 + x;
+  if (kOneRow && row >= c.rows) return;
+  const int parts = chunk_pieces(plan, chunk_keys(a, c).count());
+  const int64_t place = ((int64_t)kv * chunk_parts(plan) + part) * ws.part_rows + x;
+  float top = -INFINITY, sum = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int i = 0; i < splits; ++i) {
-    const float2 st = ws.stats[place + (int64_t)i * kChunkRows];
-    const float4 y = *reinterpret_cast<const float4*>(ws.part + (place + (int64_t)i * kChunkRows) * D + d0);
-    const float f = __builtin_amdgcn_exp2f(st.x - base);
-    sum += f * st.y;
-    acc.x += f * y.x; acc.y += f * y.y; acc.z += f * y.z; acc.w += f * y.w;
+  for (int w = kOneRow ? group : 0; w < parts && row < c.rows; w += kAtOnce * (kOneRow ? kGroups : 1)) {
+    float2 st[kAtOnce];
+    float4 y[kAtOnce];
+    float m = top;
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const int wi = w + i * (kOneRow ? kGroups : 1);
+      st[i] = make_float2(-INFINITY, 0.f);
+      y[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (wi < parts) {
+        st[i] = ws.stats[place + (int64_t)wi * ws.part_rows];
+        y[i] = *reinterpret_cast<const float4*>(ws.part + (place + (int64_t)wi * ws.part_rows) * D + d0);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) m = fmaxf(m, st[i].x);
+    const float base = m == -INFINITY ? 0.f : m, keep = __builtin_amdgcn_exp2f(top - base);
+    top = m;
+    sum *= keep;
+    acc.x *= keep; acc.y *= keep; acc.z *= keep; acc.w *= keep;
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const float f = __builtin_amdgcn_exp2f(st[i].x - base);
+      sum += f * st[i].y;
+      acc.x += f * y[i].x; acc.y += f * y[i].y; acc.z += f * y[i].z; acc.w += f * y[i].w;
+    }
+  }
+  if constexpr (kOneRow) {
+    *reinterpret_cast<float4*>(&s_acc[group][d0]) = acc;
+    if (d0 == 0) {
+      s_top[group] = top;
+      s_sum[group] = sum;
+    }
+    __syncthreads();
+    if (group != 0) return;
+#pragma unroll
+    for (int i = 1; i < kGroups; ++i) top = fmaxf(top, s_top[i]);
+    const float base = top == -INFINITY ? 0.f : top;
+    sum = 0.f;
+    acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < kGroups; ++i) {
+      const float4 y = *reinterpret_cast<const float4*>(&s_acc[i][d0]);
+      const float f = __builtin_amdgcn_exp2f(s_top[i] - base);
+      sum += f * s_sum[i];
+      acc.x += f * y.x; acc.y += f * y.y; acc.z += f * y.z; acc.w += f * y.w;
+    }
+  } else if (row >= c.rows) {
+    return;
   }
   const int tok = row / a.g, hq = kv * a.g + row - tok * a.g;
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
@@ -1185,13 +1368,21 @@ constexpr int kWorkers = 512;                             // two workgroups a CU
 struct AttnPlan {
   int step_rows;           // see AttnCall
   int mt, workers, rows;   // steps: 16-row tiles, workgroups (0: none of the call's sequences is one), rows of a kv head at most
-  int slots, splits;       // chunks: row tiles of a kv head, parts of each (0: none)
-  size_t part_bytes, chunk_part_bytes, steps_bytes, bytes;
+  int slots, splits;       // chunks: row tiles of a kv head (0: none), parts of each (0: planned on the device)
+  int chunk_workers, parts, part_rows;           // workgroups that fill the chip; parts in all and rows of a part, at most
+  size_t part_bytes, chunk_part_bytes, chunk_stats_bytes, steps_bytes, bytes;
 };
 // Which kernels a call needs.  Up to 32 rows (16 at d = 256, where two row tiles do not fit the registers) a sequence and kv
 // head is a step's.  The lengths of a ragged batch are on the device: if its longest sequence has more rows, both kernels are
 // launched, and each leaves the other's sequences; steps are then those of one row tile.
-static AttnPlan plan_of(const prism_cache* c, const prism_batch* b, int n_q_heads) {
+//
+// Row tiles of chunks are cut where they are fewer than the workgroups that fill the chip, into parts of four tiles of keys at
+// least.  The host counts them only, which is right for one sequence and for short ones.  Where a row tile may have 128 tiles of
+// keys (8192 keys, 40 us on its own) and there are several sequences, they are planned: 64 sequences of 5 tokens behind 30 to 32000,
+// d = 64, 527 -> 110 us; 4 of 40 behind 16384, 88 -> 91.  Planned always, 4 of 512 with a window of 4096 went 142 -> 150 us
+// and the ragged chunks of a windowed e4m3 batch 50 -> 56: the plan and the second look at it are two launches more.
+constexpr int kPlannedTiles = 128;
+static AttnPlan plan_of(const prism_cache* c, const prism_batch* b, int n_q_heads, int window, int sinks) {
   AttnPlan p = {};
   const int g = n_q_heads / c->n_kv_heads;
   const int64_t rows = (int64_t)b->max_tokens * g;
@@ -1212,16 +1403,21 @@ static AttnPlan plan_of(const prism_cache* c, const prism_batch* b, int n_q_head
   }
   if (!steps_only) {
     p.slots = (int)(((int64_t)b->n_tokens * g) >> 7) + b->n_seqs;
-    // parts until the chip is full, each of four tiles of keys at least
-    const int64_t tiles = (int64_t)p.slots * c->n_kv_heads, most = ((int64_t)b->max_pages * c->page + 255) / 256;
-    int64_t n = (c->head_dim == 256 ? kWorkers / 2 : kWorkers) / tiles;
-    n = n < most ? n : most;
-    p.splits = n > 1 ? (int)n : 1;
-    if (p.splits > 1) {
-      const size_t parts = (size_t)tiles * p.splits * kChunkRows;
-      p.chunk_part_bytes = align_up(parts * c->head_dim * sizeof(float), 256);
-      p.bytes = p.chunk_part_bytes + align_up(parts * sizeof(float2), 256);
+    p.chunk_workers = c->head_dim == 256 ? kWorkers / 2 : kWorkers;
+    p.part_rows = rows < kChunkRows ? (int)rows : kChunkRows;
+    const int64_t all = (int64_t)b->max_pages * c->page, band = (int64_t)window + sinks + kChunkRows;
+    const int64_t keys = window > 0 && band < all ? band : all, row_tiles = (int64_t)p.slots * c->n_kv_heads;
+    if (b->n_seqs == 1 || keys < kPlannedTiles * kChunkKeys) {
+      const int64_t n = p.chunk_workers / row_tiles, most = (keys + 4 * kChunkKeys - 1) / (4 * kChunkKeys);
+      p.splits = n <= 1 || most <= 1 ? 1 : (int)(n < most ? n : most);
+      p.parts = p.splits > 1 ? (int)row_tiles * p.splits : 0;
+    } else {
+      p.parts = (8 * p.chunk_workers + 4) / 5;                      // see chunk_plan_kernel
     }
+    const size_t part_rows = (size_t)p.parts * p.part_rows;
+    p.chunk_part_bytes = align_up(part_rows * c->head_dim * sizeof(float), 256);
+    p.chunk_stats_bytes = align_up(part_rows * sizeof(float2), 256);
+    p.bytes = 256 + p.chunk_part_bytes + p.chunk_stats_bytes + (p.splits > 0 ? 0 : align_up((4 * (size_t)p.slots + 4) * sizeof(int32_t), 256));
   }
   p.bytes += p.steps_bytes;
   return p;
@@ -1256,12 +1452,24 @@ static int launch_attn(const AttnCall& a, const AttnPlan& p, char* ws, hipStream
     if (rc != PRISM_OK || p.slots == 0) return rc;
   }
   char* cw = ws + p.steps_bytes;
-  const ChunkWs w = {reinterpret_cast<float*>(cw), reinterpret_cast<float2*>(cw + p.chunk_part_bytes)};
-  hipLaunchKernelGGL((chunk_kernel<D, kE4m3>), dim3(chunk_grid(a.cache.h_kv, p.slots, p.splits)), dim3(kChunkThreads), 0, st, a, w, p.slots,
-                     p.splits);
-  if (p.splits > 1)
-    hipLaunchKernelGGL((chunk_combine_kernel<D>), dim3(p.slots, a.cache.h_kv, kChunkRows * D / (kChunkThreads * 4)), dim3(kChunkThreads), 0, st, a,
-                       w, p.slots, p.splits);
+  int32_t* lists = reinterpret_cast<int32_t*>(cw + p.chunk_part_bytes + p.chunk_stats_bytes);
+  const size_t n = p.slots;
+  const ChunkPlan plan = {lists, lists + n + 1, lists + 2 * n + 1, lists + 3 * n + 1, lists + 4 * n + 1, p.slots, p.splits};
+  const ChunkWs w = {reinterpret_cast<float*>(cw), reinterpret_cast<float2*>(cw + p.chunk_part_bytes), plan, p.part_rows};
+  const int h_kv = a.cache.h_kv;
+  int64_t pieces = n * p.splits, joined = p.splits > 1 ? p.slots : 0;
+  if (p.splits == 0) {
+    hipLaunchKernelGGL((chunk_plan_kernel<D>), dim3(1), dim3(kPlanThreads), 0, st, a, plan, p.chunk_workers);
+    pieces = n + p.parts / h_kv + 1;
+    joined = p.parts / 2 / h_kv + 1 < p.slots ? p.parts / 2 / h_kv + 1 : p.slots;
+  }
+  hipLaunchKernelGGL((chunk_kernel<D, kE4m3>), dim3((unsigned)chunk_grid(h_kv, pieces)), dim3(kChunkThreads), 0, st, a, w);
+  if (joined == 0) return launch_status();
+  if ((int64_t)p.slots * h_kv <= 32)
+    hipLaunchKernelGGL((chunk_combine_kernel<D, true>), dim3((unsigned)joined, h_kv, p.part_rows), dim3(kChunkThreads), 0, st, a, w);
+  else
+    hipLaunchKernelGGL((chunk_combine_kernel<D, false>), dim3((unsigned)joined, h_kv, (p.part_rows * D + kChunkThreads * 4 - 1) / (kChunkThreads * 4)),
+                       dim3(kChunkThreads), 0, st, a, w);
   return launch_status();
 }
 template <int D>
@@ -1277,7 +1485,7 @@ extern "C" int prism_cache_attn_workspace_bytes(const prism_cache* cache, const 
   const int rc = check_attn(cache, batch, n_q_heads);
   if (rc != PRISM_OK) return rc;
   if (bytes == nullptr) return PRISM_ERR_INVALID_ARG;
-  *bytes = plan_of(cache, batch, n_q_heads).bytes;
+  *bytes = plan_of(cache, batch, n_q_heads, 0, 0).bytes;        // a window takes away keys, and with them parts, or the plan
   return PRISM_OK;
 }
 
@@ -1293,7 +1501,7 @@ extern "C" int prism_cache_attn(const prism_cache* cache, const prism_batch* bat
   if ((rc = check_cache_memory(cache)) != PRISM_OK || (rc = check_rows(q, h, T, d, false)) != PRISM_OK ||
       (rc = check_rows(out, h, T, d, true)) != PRISM_OK || (rc = check_in_place(q, out, h, T)) != PRISM_OK)
     return rc;
-  const AttnPlan plan = plan_of(cache, batch, h);
+  const AttnPlan plan = plan_of(cache, batch, h, params->window, params->sinks);
   if (workspace == nullptr || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < plan.bytes) return PRISM_ERR_WORKSPACE;
   const float scale = params->scale > 0.f ? params->scale : 1.f / sqrtf((float)d);
   const AttnCall a = {rows_of(q), rows_of(out), lse, cache_view(cache), batch_view(batch), h, h / cache->n_kv_heads,

@@ -13,12 +13,12 @@ pytestmark = pytest.mark.gpu
 class Case:
     """A cache with garbage (NaN) wherever no token lies, a batch and its queries, on the host and on the device."""
 
-    def __init__(self, seed, h, h_kv, d, page, e4m3, lengths, news, behind=0, how="dense", peaked=False, odd_scales=False):
+    def __init__(self, seed, h, h_kv, d, page, e4m3, lengths, news, behind=0, how="dense", peaked=False, odd_scales=False, wider=1):
         rng = np.random.default_rng(seed)
         self.lengths, self.cu = list(lengths), np.concatenate([[0], np.cumsum(news)]).astype(int)
         self.news, self.rows, self.e4m3 = list(news), int(self.cu[-1]) + behind, e4m3
         self.h, self.h_kv, self.d, self.page = h, h_kv, d, page
-        self.table, self.n_pages = su.make_table(rng, lengths, page)
+        self.table, self.n_pages = su.make_table(rng, lengths, page, wider=wider)
         shape = (self.n_pages, h_kv, page, d)
         k, v = rng.standard_normal(shape) * np.exp(0.4 * rng.standard_normal((1, h_kv, 1, d))), rng.standard_normal(shape)
         self.q = su.bf16(rng.standard_normal((h, self.rows, d)) * (3.0 if peaked else 1.2))
@@ -125,6 +125,28 @@ def test_chunks(h, h_kv, d, page, lengths, news, behind, how, e4m3):
     c.check(lse=False, scale=0.2)
     c.check(70, 5)
     c.check(17, 0)
+
+
+PLANNED = [
+    # h, h_kv, d, page, lengths, new tokens: several sequences whose tables have room for 8192 tokens and more
+    (8, 2, 128, 64, [9000, 70, 0, 300, 0], [40, 70, 9, 1, 300]),
+    (28, 4, 64, 32, [8200, 50, 1], [5, 5, 1]),
+    (16, 16, 64, 128, [200, 100, 2500], [129, 100, 20]),
+    (6, 3, 128, 64, [1500, 700], [150, 65]),
+    (4, 2, 256, 64, [8500, 10, 600], [40, 10, 33]),
+    (1, 1, 256, 32, [0, 0], [140, 30]),
+    (2, 1, 64, 64, [3000] + [5 * s % 23 for s in range(1100)], [100] + [7 * s % 20 for s in range(1100)]),
+]
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("h,h_kv,d,page,lengths,news", PLANNED)
+def test_chunks_behind_different_lengths(h, h_kv, d, page, lengths, news, e4m3):
+    c = Case(sum(news) + d, h, h_kv, d, page, e4m3, lengths, news, odd_scales=True, wider=8192 // page)
+    first, _ = c.check()
+    c.check(9000, 3, lse=False)
+    c.check(70, 5)
+    assert (su.bits(c.run()[0]) == su.bits(first)).all()
 
 
 @pytest.mark.parametrize("e4m3", [False, True])
