@@ -351,8 +351,8 @@ int prism_sparse_attn_varlen(const prism_params* params, const int32_t* cu_seqle
  * 16-byte aligned, strides are multiples of 8 and not negative; the stride of an axis of length one is not
  * looked at.  The rows of an output must not overlap: PRISM_ERR_INVALID_ARG unless one of its strides steps over
  * everything that the other axis spans.
- * Limits of a call (PRISM_ERR_UNSUPPORTED): 2^28 tokens, 2^24 sequences, 2^14 heads, 2^30 positions a sequence; for the
- * attention 2^30 rows (tokens times q-heads) and 2^24 pairs of a sequence and a kv head.
+ * Limits of a call (PRISM_ERR_UNSUPPORTED): 2^27 tokens, 2^21 sequences, 2^14 heads, 2^29 places in the pages of a sequence; for
+ * the attention 2^30 rows (tokens times q-heads) and 2^22 pairs of a sequence and a kv head.
  * ---------------------------------------------------------------------------------- */
 typedef struct prism_rows {
   void*   data;          /* device */

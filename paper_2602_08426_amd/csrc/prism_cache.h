@@ -7,8 +7,13 @@
 namespace prism {
 
 constexpr int kMaxPairs = kMaxHeadDim / 2;
-constexpr int kMaxTokens = 1 << 28;             // of a call: 32-bit row numbers and grids
-constexpr int kMaxSeqs = 1 << 24;
+// Limits of a call.  A grid's first dimension has fewer than 2^32 threads: 16 units of a token's head, 256 threads for each page of
+// up to n / 32 + 2 s, for each row tile of up to rows / 128 + pairs.  Units of 256 sequences are added in 32 bits.
+constexpr int kMaxTokens = 1 << 27;
+constexpr int kMaxSeqs = 1 << 21;
+constexpr int kMaxPlaces = 1 << 29;             // of a sequence
+constexpr int kMaxRows = 1 << 30;               // tokens times q-heads (attention)
+constexpr int kMaxSeqHeads = 1 << 22;           // pairs of a sequence and a kv head (attention)
 constexpr int kMaxHeads = 1 << 14;              // Q, K and V heads together are a grid's second dimension
 constexpr float kE4m3Max = 448.f;
 constexpr int kMinScaleExponent = -120;         // of a page and head that holds zeros only
@@ -104,7 +109,7 @@ inline int check_cache_memory(const prism_cache* c) {
 inline int check_batch(const prism_cache* c, const prism_batch* b) {
   if (b == nullptr) return PRISM_ERR_INVALID_ARG;
   if (b->n_seqs < 0 || b->n_tokens < 0 || b->max_tokens <= 0 || b->max_pages <= 0) return PRISM_ERR_INVALID_ARG;
-  if ((int64_t)b->max_pages * c->page > 1 << 30) return PRISM_ERR_UNSUPPORTED;        // positions and their sums stay in 32 bits
+  if ((int64_t)b->max_pages * c->page > kMaxPlaces) return PRISM_ERR_UNSUPPORTED;
   if (b->n_tokens > kMaxTokens || b->n_seqs > kMaxSeqs) return PRISM_ERR_UNSUPPORTED;
   if (b->n_tokens == 0) return PRISM_OK;
   if (b->n_seqs == 0 || b->lengths == nullptr || b->page_table == nullptr) return PRISM_ERR_INVALID_ARG;

@@ -3,6 +3,12 @@
 // A unit is 16 dims of one token and head: 8 pairs and two 16-byte pieces (interleaved: dims 16u .. 16u+15; half: dims
 // 8u .. 8u+7 and rot/2 + 8u ..).  A thread owns a unit of a token and goes through heads with it, so that the angles of its
 // pairs are formed once for all of them.
+//
+// Both are bound by the bytes: each value is read once and written once, and the counters show nothing beyond that.  Measured
+// (kernel alone; a large copy moves 5.0 TB/s): rotation of 32768 tokens of 28/4 heads, d = 128, 537 MB, 99 us = 5.4 TB/s; 20011 of 32/8
+// heads inside a projection, half of the dims, 410 MB, 88 us = 4.7; 32768 of 8 kv heads to bf16 pages, 268 MB, 46 us (59 in a row of calls) = 4.6;
+// 34794 of 8 kv heads to e4m3 pages and 32 q-heads, 784 MB, 65 + 109 us in the profiler, 160 in a row of calls = 4.9.  A call of one
+// token is a kernel of 4 us.
 #include "prism_cache.h"
 
 #include <cmath>

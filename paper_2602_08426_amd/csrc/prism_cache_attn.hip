@@ -14,6 +14,9 @@ constexpr float kLn2 = 0.6931471805599453f;
 
 // a value that is the same in all lanes, in a scalar register
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  return (int64_t)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x));
+}
 
 // Infinities and NaN among packed values: the top bits of theirs (bf16: an exponent of ones; e4m3: NaN, 0x7F and 0xFF), and the
 // word with zeros in their place.
@@ -82,7 +85,12 @@ __device__ __forceinline__ KeyRange key_range(const AttnCall& a, int first_pos, 
 // With the keys of S^T ordered like that, lane l holds the scores of row l%16 with keys 8*(l/16) + j, which is the B operand of
 // the second product.  A operand of V^T: a lane loads whole pieces of 8 token rows and pairs up their halves (v_perm), which
 // transposes 8 x 8 values inside the lane.  The dims of a k-step of S^T are any, as long as Q has the same: a lane's are where its
-// 16-byte pieces lie.
+// 16-byte pieces lie.  P is rounded to bf16 for the second product, 2^-8 of a probability at most; sums and maxima are fp32.
+//
+// Measured, d = 128 (kernel alone): 64 sequences of 500 to 32000 tokens, 32/8 heads, 2.06 GB of bf16 keys and values, 349 us = 5.9
+// TB/s; 8 of 128K, e4m3, 2.08 GB, 349 us = 6.0 TB/s; 16 with a window of 4096, 28/4 heads, 135 MB, 26 us = 5.2 TB/s.  A large copy
+// on this card moves 5.0 TB/s, reading alone 5.7 to 6.9; the counters show the cache's bytes read once and the matrix
+// cores busy for 4 to 8 % of the time.  One sequence of 2048 is the latency of a unit, 8 us.
 // =====================================================================================
 constexpr int kTile = 32, kStepWaves = 4;
 constexpr int kStepThreads = kStepWaves * 64;
@@ -141,7 +149,7 @@ __device__ __forceinline__ int lane_dim(int m, int i) {
 }
 
 template <int D, bool kE4m3, int MT>
-__global__ __launch_bounds__(kStepThreads, D == 256 || MT > 1 ? 1 : 2) void step_kernel(AttnCall a, StepWs ws) {
+__global__ __launch_bounds__(kStepThreads, D == 256 || (MT > 1 && !kE4m3) ? 1 : 2) void step_kernel(AttnCall a, StepWs ws) {
 #if defined(__HIP_DEVICE_COMPILE__)
   using C = StepCfg<D, kE4m3>;
   constexpr int kRow = D * C::kElem;                      // bytes of a token's row
@@ -243,7 +251,8 @@ __global__ __launch_bounds__(kStepThreads, D == 256 || MT > 1 ? 1 : 2) void step
         struct TileAt {
           int tile, page;                                 // page < 0: none
           float ks, vs;
-          __amdgpu_buffer_rsrc_t k, v;
+          int64_t off;                                    // of the tile in k and in v, and its bytes
+          int bytes;
         };
         auto locate = [&](int list_at) __attribute__((always_inline)) {
           TileAt x;
@@ -255,39 +264,41 @@ __global__ __launch_bounds__(kStepThreads, D == 256 || MT > 1 ? 1 : 2) void step
             x.ks = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, held_ks), e - held_from));
             x.vs = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, held_vs), e - held_from));
           }
-          const int64_t off = max(x.page, 0) * a.cache.page_stride + (int64_t)(kv * a.cache.page + (tok & (a.cache.page - 1))) * kRow;
-          const int bytes = x.page < 0 ? 0 : min(kTile, r.length - tok) * kRow;   // what lies behind the last token reads as zero
-          x.k = make_rsrc(a.cache.k + off, bytes);
-          x.v = make_rsrc(a.cache.v + off, bytes);
+          x.off = max(x.page, 0) * a.cache.page_stride + (int64_t)(kv * a.cache.page + (tok & (a.cache.page - 1))) * kRow;
+          x.bytes = x.page < 0 ? 0 : min(kTile, r.length - tok) * kRow;           // what lies behind the last token reads as zero
           return x;
         };
         u32x4 kw[C::kKLoads];
         uint32_t vw[8][C::kVWords];
+        // the descriptors are formed here, from scalars: kept in a TileAt they went through memory at D = 256, and a loop over the
+        // lanes' different values stood around each load
         auto load_k = [&](const TileAt& x) __attribute__((always_inline)) {
+          const __amdgpu_buffer_rsrc_t from = make_rsrc(a.cache.k + uniform(x.off), uniform(x.bytes));
 #pragma unroll
           for (int j = 0; j < C::kKLoads; ++j)
-            kw[j] = __builtin_amdgcn_raw_buffer_load_b128(x.k, k_off[j / (C::kKLoads / 2)] + (j % (C::kKLoads / 2)) * 64, 0, 0);
+            kw[j] = __builtin_amdgcn_raw_buffer_load_b128(from, k_off[j / (C::kKLoads / 2)] + (j % (C::kKLoads / 2)) * 64, 0, 0);
         };
         auto load_v = [&](const TileAt& x) __attribute__((always_inline)) {
+          const __amdgpu_buffer_rsrc_t from = make_rsrc(a.cache.v + uniform(x.off), uniform(x.bytes));
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             if constexpr (C::kVWords == 1) {
-              vw[j][0] = __builtin_amdgcn_raw_buffer_load_b32(x.v, v_off + j * kRow, 0, 0);
+              vw[j][0] = __builtin_amdgcn_raw_buffer_load_b32(from, v_off + j * kRow, 0, 0);
             } else if constexpr (C::kVWords == 2) {
-              const auto w = __builtin_amdgcn_raw_buffer_load_b64(x.v, v_off + j * kRow, 0, 0);
+              const auto w = __builtin_amdgcn_raw_buffer_load_b64(from, v_off + j * kRow, 0, 0);
               vw[j][0] = w[0];
               vw[j][1] = w[1];
             } else if constexpr (kE4m3) {                 // D = 256: two halves of 128 dims
 #pragma unroll
               for (int hf = 0; hf < 2; ++hf) {
-                const auto w = __builtin_amdgcn_raw_buffer_load_b64(x.v, v_off + j * kRow + hf * 128, 0, 0);
+                const auto w = __builtin_amdgcn_raw_buffer_load_b64(from, v_off + j * kRow + hf * 128, 0, 0);
                 vw[j][2 * hf] = w[0];
                 vw[j][2 * hf + 1] = w[1];
               }
             } else {
 #pragma unroll
               for (int hf = 0; hf < C::kVWords / 4; ++hf) {
-                const u32x4 w = __builtin_amdgcn_raw_buffer_load_b128(x.v, v_off + j * kRow + hf * 256, 0, 0);
+                const u32x4 w = __builtin_amdgcn_raw_buffer_load_b128(from, v_off + j * kRow + hf * 256, 0, 0);
                 vw[j][4 * hf] = w[0];
                 vw[j][4 * hf + 1] = w[1];
                 vw[j][4 * hf + 2] = w[2];
@@ -517,7 +528,7 @@ __global__ __launch_bounds__(kStepThreads, D == 256 || MT > 1 ? 1 : 2) void step
 
 // Joins the parts of a row that several workgroups of step_kernel worked on, and writes the rows of sequences in which no row
 // sees anything.  One workgroup a row; kGroups groups of threads take every kGroups-th part, each with a maximum of its own, so
-// that all parts are requested at once.
+// that all parts are requested at once.  Bound by latency: 3 to 7 us, of which a kernel that does nothing has 3.6 in a queue.
 template <int D, int MT>
 __global__ __launch_bounds__(kStepThreads) void combine_kernel(AttnCall a, StepWs ws, int workgroups) {
   constexpr int kGroups = kStepThreads * 4 / D;
@@ -616,6 +627,13 @@ __global__ __launch_bounds__(kStepThreads) void combine_kernel(AttnCall a, StepW
 // on the way from LDS.  bf16 pages are copied to LDS asynchronously; e4m3 pages pass through registers, where they
 // become bf16 once for the four waves (their scales go to the scores and the probabilities in fp32).
 // Rows of a kv head's q-heads lie side by side, so the 128 rows are 128 / g tokens and the diagonal costs little.
+// P is rounded to bf16 as above; sums and maxima are fp32.  The tiles are pipelined: the scores of the next tile between the
+// exponentials of this one, the second product beside the next maxima.  The running sums are scaled again only where a maximum grows by
+// more than 2^8, so exponentials are at most 2^8 (fp32 sums and bf16 P hold that as well as 1).
+//
+// Measured: 2048 tokens behind 30720, 32/8 heads, d = 128, bf16: 975 us = 1092 TFLOP/s, where a large library product
+// reaches 1379 on this card at its power limit; the matrix cores are busy for 57 % of the cycles, without bank conflicts in LDS, and the VALU
+// has most of the others (a score costs its exponential, maximum and sum whatever d is: d = 64 reaches 830 TFLOP/s).  e4m3: 1012 us.
 // Where the row tiles are few, they are cut into pieces, which chunk_combine_kernel joins: each into the same number of them, or,
 // where sequences of different lengths may be long, by chunk_plan_kernel, one workgroup, which counts the keys and deals.
 // =====================================================================================
@@ -714,7 +732,8 @@ __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(AttnCall a, Ch
   atomicAdd(&s_total, mine);                              // whole numbers: in any order
   __syncthreads();
   const unsigned long long all = s_total * a.cache.h_kv;
-  const int most = max(kLeastPiece, (int)((5 * all + 4 * workers - 1) / (4 * workers)));
+  const unsigned long long share = (5 * all + 4 * workers - 1) / (4 * workers);
+  const int most = max(kLeastPiece, (int)min(share, (unsigned long long)kMaxPlaces));
   int carry[3] = {0, 0, 0};                               // pieces, parts, cut slots in front
   for (int base = 0; base < plan.slots; base += kPlanThreads) {
     const int slot = base + t;
@@ -1373,7 +1392,8 @@ struct AttnPlan {
   size_t part_bytes, chunk_part_bytes, chunk_stats_bytes, steps_bytes, bytes;
 };
 // Which kernels a call needs.  Up to 32 rows (16 at d = 256, where two row tiles do not fit the registers) a sequence and kv
-// head is a step's.  The lengths of a ragged batch are on the device: if its longest sequence has more rows, both kernels are
+// head is a step's: us as a step / as a chunk, 64 sequences of 4096, 28 rows, d = 64 56 / 80 (e4m3 47 / 100), d = 128 107 / 114 (e4m3
+// 61 / 127); 16 of 8192, 16 rows, d = 256 190 / 192 (e4m3 103 / 174).  The lengths of a ragged batch are on the device: if its longest sequence has more rows, both kernels are
 // launched, and each leaves the other's sequences; steps are then those of one row tile.
 //
 // Row tiles of chunks are cut where they are fewer than the workgroups that fill the chip, into parts of four tiles of keys at
@@ -1395,7 +1415,10 @@ static AttnPlan plan_of(const prism_cache* c, const prism_batch* b, int n_q_head
     p.step_rows = 16 * p.mt;
     p.rows = (int)(rows < p.step_rows ? rows : p.step_rows);
     const int64_t units = (int64_t)b->n_seqs * c->n_kv_heads * (((int64_t)b->max_pages * c->page + 127) / 128);
-    const int most = c->head_dim == 256 || p.mt > 1 ? kWorkers / 2 : kWorkers;
+    // One workgroup a CU where two do not fit the registers without spilling: d = 256, and two row tiles of bf16.  us with one / two,
+    // 16 sequences of 8192, 32 rows: d = 128 bf16 106 / 132, e4m3 69 / 58; d = 64 bf16 55 / 57, e4m3 55 / 43.  d = 256, 4 rows: bf16 101 / 220,
+    // e4m3 50 / 53.
+    const int most = c->head_dim == 256 || (p.mt > 1 && c->dtype == PRISM_CACHE_BF16) ? kWorkers / 2 : kWorkers;
     p.workers = units < most ? (int)units : most;
     const size_t slots = 2 * (size_t)p.workers * 16 * p.mt;
     p.part_bytes = align_up(slots * c->head_dim * sizeof(float), 256);
@@ -1428,8 +1451,7 @@ static int check_attn(const prism_cache* cache, const prism_batch* batch, int n_
   if (rc != PRISM_OK || (rc = check_batch(cache, batch)) != PRISM_OK) return rc;
   if (n_q_heads <= 0 || n_q_heads % cache->n_kv_heads != 0) return PRISM_ERR_INVALID_ARG;
   if (n_q_heads > kMaxHeads) return PRISM_ERR_UNSUPPORTED;
-  // rows and (sequence, kv head) pairs are counted in 32 bits
-  if ((int64_t)batch->n_tokens * n_q_heads > 1 << 30 || (int64_t)batch->n_seqs * cache->n_kv_heads > 1 << 24) return PRISM_ERR_UNSUPPORTED;
+  if ((int64_t)batch->n_tokens * n_q_heads > kMaxRows || (int64_t)batch->n_seqs * cache->n_kv_heads > kMaxSeqHeads) return PRISM_ERR_UNSUPPORTED;
   return PRISM_OK;
 }
 

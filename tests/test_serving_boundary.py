@@ -62,8 +62,8 @@ BAD_CACHE = [(dict(page=16), -2), (dict(page=48), -2), (dict(page=256), -2), (di
              (dict(page_stride=1 << 60), -1)]
 BAD_MEMORY = [dict(k=None), dict(v=None), dict(k=FAKE + 2), dict(k_scale=FAKE), dict(dtype=1), dict(dtype=1, k_scale=FAKE)]
 BAD_BATCH = [(dict(n_seqs=-1), -1), (dict(n_tokens=-1), -1), (dict(max_tokens=0), -1), (dict(max_pages=0), -1), (dict(n_seqs=0), -1), (dict(lengths=None), -1),
-             (dict(page_table=None), -1), (dict(n_tokens=9), -1), (dict(max_pages=1 << 25), -2), (dict(n_tokens=(1 << 28) + 1, cu_tokens=FAKE), -2),
-             (dict(n_seqs=(1 << 24) + 1, cu_tokens=FAKE), -2)]
+             (dict(page_table=None), -1), (dict(n_tokens=9), -1), (dict(max_pages=(1 << 23) + 1), -2), (dict(n_tokens=(1 << 27) + 1, cu_tokens=FAKE), -2),
+             (dict(n_seqs=(1 << 21) + 1, cu_tokens=FAKE), -2)]
 
 
 def rotate(lib, r=None, d=128, n=10, h=4, q=None, qo=None, h_kv=2, k=None, ko=None, flags=0):
@@ -83,7 +83,7 @@ def test_rotate_refusals(lib):
         for side in ("qo", "ko"):
             assert rotate(lib, **{side: rows(data=FAKE * 2, **kw)}, n=10, h=4) == -1, (side, kw)
     assert rotate(lib, d=96) == -2 and rotate(lib, n=-1) == -1 and rotate(lib, h=-1) == -1 and rotate(lib, flags=2) == -1
-    assert rotate(lib, n=(1 << 28) + 1) == -2 and rotate(lib, h=(1 << 16) + 1) == -2
+    assert rotate(lib, n=(1 << 27) + 1) == -2 and rotate(lib, h=(1 << 16) + 1) == -2
     assert rotate(lib, q=rows(token=256, head=2560)) == -1                    # starts as its output, other strides
     assert lib.prism_rotate(ref(rotary()), 128, 10, None, 4, None, ref(rows()), 0, None, None, 0, None) == -1
 
@@ -143,6 +143,11 @@ def test_attention_refusals(lib):
     assert attn(lib, ws=None) == -3 and attn(lib, ws=FAKE + 64) == -3 and attn(lib, size=16) == -3
     assert attn(lib, q=rows(token=256, head=2560)) == -1                      # starts as its output, other strides
     assert lib.prism_cache_attn_workspace_bytes(ref(cache()), ref(batch()), 8, None) == -1
+    n = ctypes.c_size_t(0)
+    size = lambda h, **kw: lib.prism_cache_attn_workspace_bytes(ref(cache()), ref(batch(cu_tokens=FAKE, **kw)), h, ctypes.byref(n))
+    assert size(8, n_tokens=1 << 27) == 0 and size(10, n_tokens=1 << 27) == -2        # rows
+    assert size(8, n_seqs=1 << 21) == 0
+    assert lib.prism_cache_attn_workspace_bytes(ref(cache(n_kv_heads=4)), ref(batch(n_seqs=1 << 21, cu_tokens=FAKE)), 8, ctypes.byref(n)) == -2
 
 
 def test_nothing_to_do_is_no_error(lib):
