@@ -411,7 +411,8 @@ typedef struct prism_cache {
  * lengths[s] - n + i.  Token j of the sequence lies in page page_table[s * max_pages + j / page], place j % page.
  * An entry outside 0 .. n_pages-1 (say -1) is no page: its tokens are not stored and not seen; entries behind the
  * last token are not looked at.  Rows behind cu_tokens[n_seqs] are left as they were.  A position below 0 or beyond max_pages * page
- * is not stored; a query there sees what lies in front of it.  No two sequences of one call may append to the same page. */
+ * is not stored; a query there sees what lies in front of it.  The pages that a call appends to are all different ones; pages that are only read
+ * may be shared. */
 typedef struct prism_batch {
   int32_t n_seqs;
   int32_t n_tokens;            /* rows of q, k, v and out */
@@ -445,7 +446,7 @@ int prism_cache_append(const prism_cache* cache /* host */, const prism_batch* b
  * no influence.
  *   q, out : [n_q_heads, n_tokens, d]; out may be q.   lse : [n_q_heads, n_tokens] float natural-log sum-exp, or NULL.
  * workspace: prism_cache_attn_workspace_bytes() bytes; it depends on the batch's n_seqs, n_tokens, max_tokens and
- * max_pages only and carries nothing from call to call; calls that share one must not overlap.  The results do not depend
+ * max_pages and on whether it has cu_tokens (not on what lies on the device) and carries nothing from call to call; calls that share one must not overlap.  The results do not depend
  * on the order in which the device runs the parts of a call.
  * Errors: PRISM_ERR_INVALID_ARG, PRISM_ERR_UNSUPPORTED, PRISM_ERR_WORKSPACE.  n_tokens = 0 does nothing. */
 typedef struct prism_cache_attn_params {

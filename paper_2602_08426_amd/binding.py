@@ -481,7 +481,7 @@ def make_cache(k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor]
     c = prism_cache(k.data_ptr(), v.data_ptr(), _dense(k_scale, torch.float32, (n_pages, h_kv), "k_scale"),
                     _dense(v_scale, torch.float32, (n_pages, h_kv), "v_scale"), k.stride(0) if n_pages > 1 else 0, n_pages,
                     h_kv, page, d, PRISM_CACHE_E4M3 if e4m3 else PRISM_CACHE_BF16)
-    c._keep = (k, v, k_scale, v_scale)
+    c._keep, c._device = (k, v, k_scale, v_scale), k.get_device()
     return c
 
 
@@ -499,13 +499,21 @@ def make_batch(lengths: torch.Tensor, page_table: torch.Tensor, max_tokens: int 
     b = prism_batch(n, n * max_tokens if cu_tokens is None else n_tokens, max_tokens, page_table.shape[1],
                     _dense(cu_tokens, torch.int32, (n + 1,), "cu_tokens"), _dense(lengths, torch.int32, (n,), "lengths"),
                     _dense(page_table, torch.int32, page_table.shape, "page_table"))
-    b._keep = (lengths, page_table, cu_tokens)
+    b._keep, b._device = (lengths, page_table, cu_tokens), lengths.get_device()
     return b
+
+
+def _made_on_current(cache: prism_cache, batch: prism_batch) -> None:
+    here = torch._C._cuda_getDevice()
+    for s, what in ((cache, "cache"), (batch, "batch")):
+        if getattr(s, "_device", here) != here:          # descriptors filled in by hand have none
+            raise ValueError(f"the {what} is on cuda:{s._device}, calls go to the current device, cuda:{here}")
 
 
 def prism_cache_append(cache: prism_cache, batch: prism_batch, rotary: Optional[prism_rotary], k: torch.Tensor,
                        v: torch.Tensor, q_in: Optional[torch.Tensor] = None,
                        q_out: Optional[torch.Tensor] = None) -> None:
+    _made_on_current(cache, batch)
     kv = (cache.n_kv_heads, batch.n_tokens, cache.head_dim)
     heads = 0 if q_in is None else q_in.shape[0]
     q = (heads, batch.n_tokens, cache.head_dim)
@@ -524,6 +532,8 @@ def prism_cache_attn_workspace_bytes(cache: prism_cache, batch: prism_batch, n_q
 def prism_cache_attn(cache: prism_cache, batch: prism_batch, q: torch.Tensor, out: torch.Tensor,
                      lse: Optional[torch.Tensor], workspace: torch.Tensor, window: int = 0, sinks: int = 0,
                      scale: float = 0.0) -> None:
+    _made_on_current(cache, batch)
+    _on_current(workspace, workspace.dtype, "workspace")
     heads = q.shape[0]
     shape = (heads, batch.n_tokens, cache.head_dim)
     params = prism_cache_attn_params(heads, window, sinks, scale)

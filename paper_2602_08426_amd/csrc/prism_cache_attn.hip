@@ -1523,11 +1523,13 @@ extern "C" int prism_cache_attn(const prism_cache* cache, const prism_batch* bat
   if ((rc = check_cache_memory(cache)) != PRISM_OK || (rc = check_rows(q, h, T, d, false)) != PRISM_OK ||
       (rc = check_rows(out, h, T, d, true)) != PRISM_OK || (rc = check_in_place(q, out, h, T)) != PRISM_OK)
     return rc;
-  const AttnPlan plan = plan_of(cache, batch, h, params->window, params->sinks);
+  // positions lie between -2^27 and 2^30: a window that is longer sees as much, and position - window stays in 32 bits
+  const int window = params->window < 1 << 30 ? params->window : 1 << 30;
+  const AttnPlan plan = plan_of(cache, batch, h, window, params->sinks);
   if (workspace == nullptr || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < plan.bytes) return PRISM_ERR_WORKSPACE;
   const float scale = params->scale > 0.f ? params->scale : 1.f / sqrtf((float)d);
   const AttnCall a = {rows_of(q), rows_of(out), lse, cache_view(cache), batch_view(batch), h, h / cache->n_kv_heads,
-                      params->window, params->sinks, scale * kLog2e, plan.step_rows};
+                      window, params->sinks, scale * kLog2e, plan.step_rows};
   const bool e4m3 = cache->dtype == PRISM_CACHE_E4M3;
   char* ws = static_cast<char*>(workspace);
   hipStream_t st = static_cast<hipStream_t>(stream);

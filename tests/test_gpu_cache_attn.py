@@ -166,6 +166,7 @@ def test_length_smaller_than_new_tokens(e4m3):
         c.q = su.bf16(np.random.default_rng(1).standard_normal((4, c.rows, 64)))
         c.qd = su.to_device(c.q)
         c.check()
+        c.check(2 ** 31 - 1, 2 ** 31 - 1)
 
 
 @pytest.mark.parametrize("e4m3", [False, True])

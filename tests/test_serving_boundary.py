@@ -156,6 +156,17 @@ def test_nothing_to_do_is_no_error(lib):
     assert rotate(lib, n=0) == 0 and rotate(lib, h=0, h_kv=0) == 0
 
 
+def test_binding_refuses_descriptors_of_another_device(monkeypatch):
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0)
+    x = torch.zeros((2, 10, 128), dtype=torch.bfloat16)
+    for there in ((1, 0), (0, 1)):
+        c, b = cache(), batch()
+        c._device, b._device = there
+        for call in (lambda: pb.prism_cache_append(c, b, None, x, x), lambda: pb.prism_cache_attn(c, b, x, x, None, x)):
+            with pytest.raises(ValueError, match="current device"):
+                call()
+
+
 def test_binding_refuses_what_is_not_on_the_device():
     x = torch.zeros((2, 3, 64), dtype=torch.bfloat16)
     with pytest.raises(ValueError):
