@@ -1393,8 +1393,12 @@ struct AttnPlan {
 };
 // Which kernels a call needs.  Up to 32 rows (16 at d = 256, where two row tiles do not fit the registers) a sequence and kv
 // head is a step's: us as a step / as a chunk, 64 sequences of 4096, 28 rows, d = 64 56 / 80 (e4m3 47 / 100), d = 128 107 / 114 (e4m3
-// 61 / 127); 16 of 8192, 16 rows, d = 256 190 / 192 (e4m3 103 / 174).  The lengths of a ragged batch are on the device: if its longest sequence has more rows, both kernels are
-// launched, and each leaves the other's sequences; steps are then those of one row tile.
+// 61 / 127); 16 of 8192, 16 rows, d = 256 190 / 192 (e4m3 103 / 174).  The lengths of a ragged batch are on the device: if its longest
+// sequence has more rows, all are a chunk's, single tokens in row tiles of their own beside the others, as long as the sequences
+// are short (below) and do not fill the chip by themselves; otherwise both kernels are launched, and each leaves the
+// other's sequences; steps are then those of one row tile.  us with one / both kernels, a chunk of 512 tokens and single ones of others: 7 of
+// 1024 (window), 32/8 heads, d = 128 35 / 46 (e4m3 39 / 48), 63 of them 87 / 90 (87 / 76); 7 of 8100 119 / 138 (132 / 136); 7 of 16000
+// 259 / 238 (283 / 200), 31 of them 551 / 486 (437 / 339).
 //
 // Row tiles of chunks are cut where they are fewer than the workgroups that fill the chip, into parts of four tiles of keys at
 // least.  The host counts them only, which is right for one sequence and for short ones.  Where a row tile may have 128 tiles of
@@ -1410,7 +1414,11 @@ static AttnPlan plan_of(const prism_cache* c, const prism_batch* b, int n_q_head
   if (b->n_seqs == 0 || b->n_tokens == 0) return p;
   const bool steps_only = rows <= (c->head_dim == 256 ? 16 : 32);
   const bool ragged = b->cu_tokens != nullptr && b->n_seqs > 1;
-  if (steps_only || (ragged && g <= 16)) {
+  const int64_t all = (int64_t)b->max_pages * c->page, band = (int64_t)window + sinks + kChunkRows;
+  const int64_t keys = window > 0 && band < all ? band : all;
+  const bool planned = b->n_seqs > 1 && keys >= kPlannedTiles * kChunkKeys;
+  p.chunk_workers = c->head_dim == 256 ? kWorkers / 2 : kWorkers;
+  if (steps_only || (ragged && g <= 16 && (planned || (int64_t)b->n_seqs * c->n_kv_heads >= p.chunk_workers))) {
     p.mt = steps_only && rows > 16 ? 2 : 1;
     p.step_rows = 16 * p.mt;
     p.rows = (int)(rows < p.step_rows ? rows : p.step_rows);
@@ -1426,11 +1434,9 @@ static AttnPlan plan_of(const prism_cache* c, const prism_batch* b, int n_q_head
   }
   if (!steps_only) {
     p.slots = (int)(((int64_t)b->n_tokens * g) >> 7) + b->n_seqs;
-    p.chunk_workers = c->head_dim == 256 ? kWorkers / 2 : kWorkers;
     p.part_rows = rows < kChunkRows ? (int)rows : kChunkRows;
-    const int64_t all = (int64_t)b->max_pages * c->page, band = (int64_t)window + sinks + kChunkRows;
-    const int64_t keys = window > 0 && band < all ? band : all, row_tiles = (int64_t)p.slots * c->n_kv_heads;
-    if (b->n_seqs == 1 || keys < kPlannedTiles * kChunkKeys) {
+    const int64_t row_tiles = (int64_t)p.slots * c->n_kv_heads;
+    if (!planned) {
       const int64_t n = p.chunk_workers / row_tiles, most = (keys + 4 * kChunkKeys - 1) / (4 * kChunkKeys);
       p.splits = n <= 1 || most <= 1 ? 1 : (int)(n < most ? n : most);
       p.parts = p.splits > 1 ? (int)row_tiles * p.splits : 0;

@@ -125,6 +125,8 @@ def test_chunks(h, h_kv, d, page, lengths, news, behind, how, e4m3):
     c.check(lse=False, scale=0.2)
     c.check(70, 5)
     c.check(17, 0)
+    if len(lengths) > 1:                           # tables for 8192 tokens: single tokens apart from chunks, chunks cut by their keys
+        Case(sum(news) + d, h, h_kv, d, page, e4m3, lengths, news, behind, how, odd_scales=True, wider=8192 // page).check()
 
 
 PLANNED = [
@@ -271,6 +273,34 @@ def test_graphs_share_a_workspace_and_follow_the_lengths(news, e4m3):
         for x, a in ((c, args[0]), (e, args[1])):
             su.check_attention(su.host(a[3]), a[4].double().cpu().numpy(), x.q, x.k, x.v, x.lengths, x.cu, x.table, 100, 4)
         e.run(100, 4, workspace=ws)
+
+
+@pytest.mark.parametrize("window", [0, 300])
+def test_graph_of_a_ragged_batch_follows_the_lengths(window):
+    """Lengths and offsets change between the replays; tables are wide enough for a plan on the device (window 0)."""
+    c = Case(73, 8, 2, 128, 64, False, [1500, 700, 90], [50, 1, 33], behind=44, wider=128)
+    cache = pb.make_cache(c.kd, c.vd)
+    batch = pb.make_batch(su.ints(c.lengths), su.ints(c.table), 64, su.ints(c.cu), c.rows)
+    out, lse = torch.empty_like(c.qd), torch.empty((c.h, c.rows), device="cuda")
+    ws = pb.alloc_workspace(pb.prism_cache_attn_workspace_bytes(cache, batch, c.h))
+    pb.prism_cache_attn(cache, batch, c.qd, out, lse, ws, window, 4)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        pb.prism_cache_attn(cache, batch, c.qd, out, lse, ws, window, 4)
+    for lengths, news in (([1500, 700, 90], [50, 1, 33]), ([1400, 30, 90], [1, 30, 64]), ([64, 699, 0], [64, 60, 0]), ([0, 0, 1], [0, 0, 1])):
+        c.lengths, c.cu = lengths, np.concatenate([[0], np.cumsum(news)])
+        batch._keep[0].copy_(su.ints(lengths))
+        batch._keep[2].copy_(su.ints(c.cu))
+        out.fill_(7.0)
+        lse.fill_(7.0)
+        ws.fill_(0xFF)
+        graph.replay()
+        torch.cuda.synchronize()
+        o, l = su.host(out), lse.double().cpu().numpy()
+        mine = su.check_attention(o, l, c.q, c.k, c.v, c.lengths, c.cu, c.table, window, 4)
+        assert (o[~mine] == 7.0).all() and (l[~mine] == 7.0).all()
 
 
 def test_another_stream():
