@@ -631,7 +631,7 @@ __global__ __launch_bounds__(kStepThreads) void combine_kernel(AttnCall a, StepW
 // exponentials of this one, the second product beside the next maxima.  The running sums are scaled again only where a maximum grows by
 // more than 2^8, so exponentials are at most 2^8 (fp32 sums and bf16 P hold that as well as 1).
 //
-// Measured: 2048 tokens behind 30720, 32/8 heads, d = 128, bf16: 975 us = 1092 TFLOP/s, where a large library product
+// Measured: 2048 tokens behind 30720, 32/8 heads, d = 128, bf16: 975 to 1049 us by the card = 1092 to 1015 TFLOP/s, where a large library product
 // reaches 1379 on this card at its power limit; the matrix cores are busy for 57 % of the cycles, without bank conflicts in LDS, and the VALU
 // has most of the others (a score costs its exponential, maximum and sum whatever d is: d = 64 reaches 830 TFLOP/s).  e4m3: 1012 us.
 // Where the row tiles are few, they are cut into pieces, which chunk_combine_kernel joins: each into the same number of them, or,
